@@ -459,6 +459,102 @@ ft_status ft_stream_rate(const void *src, void *dst, uint64_t bytes, uint32_t it
 ft_status ft_launch_timed_graph(const ft_plan *plan, const void *const *A, const void *const *B, void *const *C,
                                 uint32_t n_sets, void *hip_stream, uint32_t iters, float *ms_per_launch);
 
+/* ---------------------------------------------------------------------------------------
+ * (e) Matmuls in 8-bit integers, and tokens sorted by expert (Sec. 3's contractions where the
+ * operands have 8 bits, and where the extents of a grouped launch are known on the device only).
+ *
+ * All calls: device pointers owned by the caller, hip_stream a hipStream_t (NULL = default stream) of the
+ * current HIP device, on which the operands live (a stream of another device: FT_ERR_INVALID_ARG).
+ * Asynchronous; they allocate nothing, keep nothing between calls, do not synchronise and may be captured
+ * into a graph.  Outputs must not overlap inputs.  Descriptors are host pointers, read during the call only.
+ * The same call on the same values gives the same bits, whatever stream or address.
+ * ------------------------------------------------------------------------------------- */
+enum { FT_F32 = 2 };               /* element type of ft_quant_desc and ft_expert_desc only  */
+enum { FT_ACT_NONE = 0, FT_ACT_SILU_MUL = 1 };
+enum { FT_EPI_SILU_MUL = 2 };      /* epilogue of ft_i8_desc only                            */
+
+/* Rows of values as 8-bit integers with one scale each.  f = X[i, 0 .. cols), or with FT_ACT_SILU_MUL
+ * f[j] = g / (1 + exp(-g)) * u for g = X[i, j], u = X[i, cols + j] (in fp32, not rounded to 16 bits):
+ *   scale[i] = max_j |f[j]| / 127,  Q[i, j] = 127 f[j] / max_j |f[j]| rounded to nearest, ties to even
+ * -- exactly so for 16-bit values without an activation; else in fp32, so that a value beside the middle
+ * between two integers may be one off.  A row of zeros has scale 0 and zeros; a row that holds an infinity or a NaN (or
+ * whose f does) has scale NaN and zeros, so that what is computed from it is NaN.  Bytes of Q between cols and
+ * ldq are set to zero. */
+typedef struct ft_quant_desc {
+    uint32_t struct_size;
+    uint32_t cols;                 /* integers of a row, 1 .. 2^20                           */
+    uint32_t ldx;                  /* row pitch of X in elements; 0: densely packed (cols, or 2 * cols with an activation) */
+    uint32_t ldq;                  /* row pitch of Q in bytes, a multiple of 16; 0: cols rounded up to one */
+    uint32_t dtype;                /* FT_F16, FT_BF16 or FT_F32                              */
+    uint32_t act;                  /* FT_ACT_*                                               */
+} ft_quant_desc;
+/* X: aligned to its elements (rows on 16-byte blocks are read fastest).  Q: 16-byte aligned, rows x ldq bytes.  scale: rows fp32 values. */
+ft_status ft_i8_quantize(const ft_quant_desc *desc, uint32_t rows, const void *X, int8_t *Q, float *scale, void *hip_stream);
+
+/* Matmul of 8-bit integers with a scale for each row of A (token) and each row of B (channel):
+ *   C[i, j] = scale_a[i] * scale_b[j] * sum_k A[i, k] B[j, k] (+ bias[j])
+ * B is stored [N][K] (FT_B_NK).  The sum is an exact 32-bit integer (k <= 131071), the rest is fp32, rounded once where C has 16 bits.
+ * With FT_EPI_SILU_MUL the n columns are n / 2 gates and n / 2 values, and C has n / 2 columns: C[i, j] = g / (1 + exp(-g)) * p[i, n / 2 + j] for
+ * the products p above and g = p[i, j].  (A C of 16 bits that is quantised again loses more than its own rounding: the integers beside the
+ * middle between two fall to another side.  Keep FT_OUT_F32 there.) */
+typedef struct ft_i8_desc {
+    uint32_t struct_size;
+    uint32_t n, k;                 /* n: 1 .. 2^20 - 1, even with FT_EPI_SILU_MUL; k: 1 .. 131071 */
+    uint32_t lda, ldb;             /* row pitches of A and B in bytes, multiples of 16, at most 2^20; 0: k rounded up to one.
+                                      Whole pitches are read; what lies between k and the pitch does not matter */
+    uint32_t ldc;                  /* row pitch of C in elements, at most 2^22; 0: C's columns. Elements beyond them are not written */
+    uint32_t dtype;                /* FT_F16 / FT_BF16: the 16-bit type of FT_OUT_SAME        */
+    uint32_t out_dtype;            /* FT_OUT_*                                               */
+    uint32_t epilogue;             /* FT_EPI_NONE, FT_EPI_BIAS or FT_EPI_SILU_MUL            */
+    uint32_t experts;              /* ft_i8_matmul: 0. ft_i8_matmul_experts: weights of B, 1 .. 1024 */
+} ft_i8_desc;
+/* A [m][lda], B [n][ldb]: 16-byte aligned, all rows with whole pitches.  scale_a [m], scale_b [n], bias [n]: fp32; bias non-NULL
+ * exactly with FT_EPI_BIAS.  C [m][ldc]: aligned to its elements (rows on 16-byte blocks are written fastest).  m = 0 launches nothing. */
+ft_status ft_i8_matmul(const ft_i8_desc *desc, uint32_t m, const int8_t *A, const float *scale_a, const int8_t *B, const float *scale_b,
+                       const float *bias, void *C, void *hip_stream);
+/* The same for rows sorted by expert, in one launch whose group sizes are read on the device: rows offsets[e] .. offsets[e + 1] of C
+ * are products with weight e of B [experts][n][ldb], scale_b [experts][n], bias [experts][n].  offsets: experts + 1 ascending
+ * values (device, as ft_expert_sort leaves them); values beyond rows count as rows, descending ones as empty groups.  Row r of C is of row
+ * a_row[r] of A (device, e.g. row_token of ft_expert_sort: no gathered copy of A is needed), or of row r where a_row is NULL; A and
+ * scale_a have a_rows rows, and a row outside of them counts as zeros.  Rows of C before offsets[0] and from offsets[experts] on are left as they were.
+ * a_rows * lda < 2^31 and rows < 2^31, else FT_ERR_UNSUPPORTED.  rows = 0 launches nothing. */
+ft_status ft_i8_matmul_experts(const ft_i8_desc *desc, uint32_t rows, const int32_t *offsets, const int8_t *A, const float *scale_a,
+                               const int32_t *a_row, uint32_t a_rows, const int8_t *B, const float *scale_b, const float *bias, void *C,
+                               void *hip_stream);
+
+/* Tokens sorted by expert and back.  An entry (t, j), t < tokens, j < top_k, is one of the experts of token t; its id is
+ * expert_of[t * top_k + j], and an id outside of 0 .. experts - 1 (e.g. -1 for padding) means none. */
+typedef struct ft_expert_desc {
+    uint32_t struct_size;
+    uint32_t experts;              /* 1 .. 1024                                              */
+    uint32_t top_k;                /* 1 .. 32                                                */
+    uint32_t cols;                 /* elements of a token's row, 1 .. 2^20; ft_expert_sort does not look at it, nor at the following */
+    uint32_t ld_token;             /* row pitch in elements of what has a row for each token (X, Out, dOut); 0: cols */
+    uint32_t ld_row;               /* row pitch in elements of what has a row for each entry (Y, dY); 0: cols */
+    uint32_t dtype;                /* FT_F16, FT_BF16 or FT_F32                              */
+} ft_expert_desc;
+/* Bytes of workspace that ft_expert_sort needs (0: none). *bytes: host pointer. */
+ft_status ft_expert_workspace(const ft_expert_desc *desc, uint32_t tokens, uint64_t *bytes);
+/* Sorts the entries by expert, those of one expert in the order of the entries: offsets [experts + 1] where each expert's rows
+ * begin, row_token [tokens * top_k] the token of each row (-1 from row offsets[experts] on), row_of [tokens * top_k] the row of each entry (-1:
+ * none).  workspace: device, 16-byte aligned, at least as many bytes as ft_expert_workspace says, its contents do not matter; calls that may overlap in
+ * time need one each.  tokens * top_k < 2^31.  With tokens = 0 all offsets are 0. */
+ft_status ft_expert_sort(const ft_expert_desc *desc, uint32_t tokens, const int32_t *expert_of, int32_t *offsets, int32_t *row_token,
+                         int32_t *row_of, void *workspace, uint64_t workspace_bytes, void *hip_stream);
+/* Carries the tokens to their rows: Y[row_of[t, j]] = X[t].  Rows that no entry has are left as they were.  An entry of row_of
+ * outside of 0 .. tokens * top_k - 1 counts as none, here and below; no two entries may have the same row.
+ * The gradient by X is ft_expert_combine of the gradient by Y without weights. */
+ft_status ft_expert_gather(const ft_expert_desc *desc, uint32_t tokens, const void *X, const int32_t *row_of, void *Y, void *hip_stream);
+/* ... and back: Out[t] = sum_j weights[t, j] * Y[row_of[t, j]], summed in fp32 by ascending j and rounded once; entries without a row add
+ * nothing, whatever their weight.  weights: [tokens * top_k] fp32, or NULL for ones. */
+ft_status ft_expert_combine(const ft_expert_desc *desc, uint32_t tokens, const void *Y, const int32_t *row_of, const float *weights,
+                            void *Out, void *hip_stream);
+/* Gradients of ft_expert_combine: dY[row_of[t, j]] = weights[t, j] * dOut[t], and dweights[t, j] = the sum over the columns of
+ * dOut[t] * Y[row_of[t, j]] in fp32 (0 for an entry without a row).  dweights may be NULL (Y is not read then, and may be NULL too);
+ * weights may be NULL for ones. */
+ft_status ft_expert_combine_grad(const ft_expert_desc *desc, uint32_t tokens, const void *dOut, const void *Y, const int32_t *row_of,
+                                 const float *weights, void *dY, float *dweights, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

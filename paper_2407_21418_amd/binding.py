@@ -32,6 +32,9 @@ FT_B_KN, FT_B_NK = 0, 1
 FT_PLAN_PATCHWORK, FT_PLAN_PAD_BASELINE, FT_PLAN_FORCED, FT_PLAN_HOST_ONLY, FT_PLAN_TABLE_ORDER = 0, 1, 2, 16, 32
 FT_SIA_LINEAR, FT_SIA_PRODUCT = 0, 1
 FT_FORM_TILES, FT_FORM_ROWS, FT_FORM_BLOCKS, FT_FORM_PATCHES, FT_FORM_GRID = 0, 1, 2, 3, 4
+FT_F32 = 2                            # ft_quant_desc and ft_expert_desc only
+FT_ACT_NONE, FT_ACT_SILU_MUL = 0, 1
+FT_EPI_SILU_MUL = 2                   # ft_i8_desc only
 
 u32, u64, u16 = C.c_uint32, C.c_uint64, C.c_uint16
 
@@ -105,6 +108,18 @@ class ft_pool_entry(C.Structure):
                 ("occ_q20", u32), ("cmr_q20", u32), ("flags", u32), ("sia_q20", u64), ("n_tiles", u64)]
 
 
+class ft_quant_desc(_S):
+    _fields_ = [(n, u32) for n in ("struct_size", "cols", "ldx", "ldq", "dtype", "act")]
+
+
+class ft_i8_desc(_S):
+    _fields_ = [(n, u32) for n in ("struct_size", "n", "k", "lda", "ldb", "ldc", "dtype", "out_dtype", "epilogue", "experts")]
+
+
+class ft_expert_desc(_S):
+    _fields_ = [(n, u32) for n in ("struct_size", "experts", "top_k", "cols", "ld_token", "ld_row", "dtype")]
+
+
 class FtError(RuntimeError):
     def __init__(self, status, what):
         self.status = status
@@ -145,6 +160,14 @@ SYMBOLS = {
                                     C.POINTER(C.c_float)]),
     "ft_launch_timed_graph": (C.c_int32, [_P, C.POINTER(_P), C.POINTER(_P), C.POINTER(_P), u32, _P, u32,
                                           C.POINTER(C.c_float)]),
+    "ft_i8_quantize": (C.c_int32, [C.POINTER(ft_quant_desc), u32, _P, _P, _P, _P]),
+    "ft_i8_matmul": (C.c_int32, [C.POINTER(ft_i8_desc), u32, _P, _P, _P, _P, _P, _P, _P]),
+    "ft_i8_matmul_experts": (C.c_int32, [C.POINTER(ft_i8_desc), u32, _P, _P, _P, _P, u32, _P, _P, _P, _P, _P]),
+    "ft_expert_workspace": (C.c_int32, [C.POINTER(ft_expert_desc), u32, C.POINTER(u64)]),
+    "ft_expert_sort": (C.c_int32, [C.POINTER(ft_expert_desc), u32, _P, _P, _P, _P, _P, u64, _P]),
+    "ft_expert_gather": (C.c_int32, [C.POINTER(ft_expert_desc), u32, _P, _P, _P, _P]),
+    "ft_expert_combine": (C.c_int32, [C.POINTER(ft_expert_desc), u32, _P, _P, _P, _P, _P]),
+    "ft_expert_combine_grad": (C.c_int32, [C.POINTER(ft_expert_desc), u32, _P, _P, _P, _P, _P, _P, _P]),
 }
 
 
@@ -365,6 +388,52 @@ def ft_launch_timed(p: Plan, A, B, Cs, stream: int, iters: int, graph: bool = Fa
     _check(fn(p.ptr, arr(A), arr(B), arr(Cs), n, stream, iters, C.byref(ms)),
            "ft_launch_timed_graph" if graph else "ft_launch_timed")
     return ms.value
+
+
+def ft_i8_quantize(desc: ft_quant_desc, rows: int, X: int, Q: int, scale: int, stream: int = 0):
+    """Rows of values at X as 8-bit integers at Q with one fp32 scale each.  All addresses here and below: device
+    addresses (0 / None for none); stream: hipStream_t value."""
+    _check(lib().ft_i8_quantize(C.byref(desc), rows, X, Q, scale, stream), "ft_i8_quantize")
+
+
+def ft_i8_matmul(desc: ft_i8_desc, m: int, A: int, scale_a: int, B: int, scale_b: int, bias: int, Cptr: int, stream: int = 0):
+    """C[i, j] = scale_a[i] * scale_b[j] * sum_k A[i, k] B[j, k] (+ bias[j]) of 8-bit integers; B is stored [n][k]."""
+    _check(lib().ft_i8_matmul(C.byref(desc), m, A, scale_a, B, scale_b, bias or None, Cptr, stream), "ft_i8_matmul")
+
+
+def ft_i8_matmul_experts(desc: ft_i8_desc, rows: int, offsets: int, A: int, scale_a: int, a_row: int, a_rows: int, B: int, scale_b: int, bias: int,
+                         Cptr: int, stream: int = 0):
+    """The same where rows offsets[e] .. offsets[e + 1] of C belong to weight e; row r is of row a_row[r] of A (a_row 0: of row r)."""
+    _check(lib().ft_i8_matmul_experts(C.byref(desc), rows, offsets, A, scale_a, a_row or None, a_rows, B, scale_b, bias or None, Cptr, stream),
+           "ft_i8_matmul_experts")
+
+
+def ft_expert_workspace(desc: ft_expert_desc, tokens: int) -> int:
+    """Bytes of workspace of ft_expert_sort."""
+    n = u64()
+    _check(lib().ft_expert_workspace(C.byref(desc), tokens, C.byref(n)), "ft_expert_workspace")
+    return n.value
+
+
+def ft_expert_sort(desc: ft_expert_desc, tokens: int, expert_of: int, offsets: int, row_token: int, row_of: int, workspace: int, workspace_bytes: int,
+                   stream: int = 0):
+    """Rows of the entries sorted by expert: where each expert's begin, the token of each row, the row of each entry."""
+    _check(lib().ft_expert_sort(C.byref(desc), tokens, expert_of, offsets, row_token, row_of, workspace or None, workspace_bytes, stream), "ft_expert_sort")
+
+
+def ft_expert_gather(desc: ft_expert_desc, tokens: int, X: int, row_of: int, Y: int, stream: int = 0):
+    """Y[row_of[t, j]] = X[t]."""
+    _check(lib().ft_expert_gather(C.byref(desc), tokens, X, row_of, Y, stream), "ft_expert_gather")
+
+
+def ft_expert_combine(desc: ft_expert_desc, tokens: int, Y: int, row_of: int, weights: int, Out: int, stream: int = 0):
+    """Out[t] = sum_j weights[t, j] * Y[row_of[t, j]] (weights 0: ones)."""
+    _check(lib().ft_expert_combine(C.byref(desc), tokens, Y, row_of, weights or None, Out, stream), "ft_expert_combine")
+
+
+def ft_expert_combine_grad(desc: ft_expert_desc, tokens: int, dOut: int, Y: int, row_of: int, weights: int, dY: int, dweights: int, stream: int = 0):
+    """Gradients of ft_expert_combine by Y and by the weights (dweights 0: not wanted, Y is not read then)."""
+    _check(lib().ft_expert_combine_grad(C.byref(desc), tokens, dOut, Y or None, row_of, weights or None, dY, dweights or None, stream), "ft_expert_combine_grad")
 
 
 # A serving loop makes these three for every Matmul: the native ones read the usual arguments themselves and hand every other call to

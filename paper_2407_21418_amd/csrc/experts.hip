@@ -1,0 +1,386 @@
+// Tokens sorted by expert and back.
+//
+// The sort is a counting sort that keeps the order of the entries: row = rows of lower experts + earlier entries of the same
+// expert.  A wave counts 64 entries at a time (those of one id find each other with a ballot for each bit of the id), every wave
+// of a workgroup has counts of its own for its stretch of the entries, and their prefix sums give each wave the row
+// where its next entry of an expert goes.  No atomic decides an order.
+//
+// The moves are bound by memory: a workgroup's threads hold a token's row in pieces of 16 bytes and read or write it once
+// for all of its entries; rows of entries are read or written once.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "ft_internal.h"
+#include "i8_ops.h"
+#include "lane_types.h"
+#include "op_launch.h"
+
+namespace ftk {
+
+struct SortArgs {
+    const int32_t *ids;
+    int32_t *offsets, *row_token, *row_of;
+    uint32_t *counts;                    // [blocks][experts], more than one block only
+    uint32_t n, experts, top_k;
+    uint32_t blocks, per_block;          // entries of a block
+    uint32_t id_bits;                    // bits of experts - 1
+};
+
+// this wave's count of every id among its stretch [s0, s1) of the entries
+__device__ __forceinline__ void count_stretch(const SortArgs &a, uint32_t s0, uint32_t s1, uint32_t lane, uint32_t *mine) {
+    for (uint32_t i = s0 + lane; i < s1; i += 64u) {
+        const uint32_t id = (uint32_t)a.ids[i];
+        if (id < a.experts) atomicAdd(&mine[id], 1u);
+    }
+}
+// exclusive prefix sums of v[0 .. n) by one wave, in place; v[n] receives the total
+__device__ __forceinline__ void scan_by_wave(uint32_t *v, uint32_t n, uint32_t lane) {
+    uint32_t carry = 0;
+    for (uint32_t at = 0; at < n; at += 64u) {
+        const uint32_t x = at + lane < n ? v[at + lane] : 0u;
+        uint32_t sum = x;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const uint32_t up = __shfl_up(sum, d);
+            if (lane >= (uint32_t)d) sum += up;
+        }
+        if (at + lane < n) v[at + lane] = carry + sum - x;
+        carry += __shfl(sum, 63);
+    }
+    if (lane == 0) v[n] = carry;
+}
+
+// Stretches of a block's entries: whole steps of 64, one for each wave.
+__device__ __forceinline__ void stretch_of(const SortArgs &a, uint32_t wave, uint32_t waves, uint32_t *s0, uint32_t *s1) {
+    const uint32_t b0 = blockIdx.x * a.per_block, b1 = a.n - b0 < a.per_block ? a.n : b0 + a.per_block;
+    const uint32_t steps = (b1 - b0 + 63u) / 64u, per = (steps + waves - 1u) / waves * 64u;
+    *s0 = b1 - b0 < wave * per ? b1 : b0 + wave * per;
+    *s1 = b1 - *s0 < per ? b1 : *s0 + per;
+}
+
+// counts[block][expert] of more than one block
+__global__ __launch_bounds__(1024) void ft_expert_count(SortArgs a) {
+    extern __shared__ uint32_t lds[];
+    const uint32_t tid = threadIdx.x, threads = blockDim.x;
+    for (uint32_t e = tid; e < a.experts; e += threads) lds[e] = 0u;
+    __syncthreads();
+    uint32_t s0, s1;
+    stretch_of(a, tid / 64u, threads / 64u, &s0, &s1);
+    count_stretch(a, s0, s1, tid & 63u, lds);
+    __syncthreads();
+    for (uint32_t e = tid; e < a.experts; e += threads) a.counts[(uint64_t)blockIdx.x * a.experts + e] = lds[e];
+}
+
+__global__ __launch_bounds__(1024) void ft_expert_place(SortArgs a) {
+    // cnt [waves][experts], first [experts + 1], below [experts]
+    extern __shared__ uint32_t lds[];
+    const uint32_t tid = threadIdx.x, threads = blockDim.x, lane = tid & 63u, wave = tid / 64u, waves = threads / 64u, E = a.experts;
+    uint32_t *const cnt = lds, *const first = lds + waves * E, *const below = first + E + 1u, *const mine = cnt + wave * E;
+    for (uint32_t i = tid; i < waves * E; i += threads) cnt[i] = 0u;
+    for (uint32_t e = tid; e < E; e += threads) first[e] = below[e] = 0u;
+    __syncthreads();
+    uint32_t s0, s1;
+    stretch_of(a, wave, waves, &s0, &s1);
+    count_stretch(a, s0, s1, lane, mine);
+    if (a.blocks > 1u) {
+        // all blocks' counts, and those of the blocks before this one; parts of the threads take turns with the blocks
+        const uint32_t parts = threads / E ? threads / E : 1u;
+        for (uint32_t i = tid; i < parts * E; i += threads) {
+            const uint32_t e = i % E;
+            uint32_t all = 0, before = 0;
+            for (uint32_t b = i / E; b < a.blocks; b += parts) {
+                const uint32_t c = a.counts[(uint64_t)b * E + e];
+                all += c;
+                before += b < blockIdx.x ? c : 0u;
+            }
+            atomicAdd(&first[e], all);
+            atomicAdd(&below[e], before);
+        }
+    }
+    __syncthreads();
+    // the waves' counts to prefix sums over the waves
+    for (uint32_t e = tid; e < E; e += threads) {
+        uint32_t sum = 0;
+        for (uint32_t w = 0; w < waves; ++w) {
+            const uint32_t c = cnt[w * E + e];
+            cnt[w * E + e] = sum;
+            sum += c;
+        }
+        if (a.blocks == 1u) first[e] = sum;
+    }
+    __syncthreads();
+    if (wave == 0) scan_by_wave(first, E, lane);
+    __syncthreads();
+    if (blockIdx.x == 0)
+        for (uint32_t e = tid; e <= E; e += threads) a.offsets[e] = (int32_t)first[e];
+    for (uint32_t e = lane; e < E; e += 64u) mine[e] += first[e] + below[e];
+    // (a wave's LDS accesses are in order: what follows touches its own counts only)
+    __builtin_amdgcn_wave_barrier();
+    for (uint32_t at = s0; at < s1; at += 64u) {
+        const uint32_t i = at + lane;
+        const uint32_t id = i < s1 ? (uint32_t)a.ids[i] : ~0u;
+        const bool has = id < E;
+        uint64_t peers = __ballot(has);
+        for (uint32_t bit = 0; bit < a.id_bits; ++bit) {
+            const uint64_t set = __ballot((id >> bit) & 1u);
+            peers &= (id >> bit) & 1u ? set : ~set;
+        }
+        const uint32_t rank = __builtin_popcountll(peers & ((1ull << lane) - 1ull));
+        uint32_t row = 0;
+        if (has) row = mine[id] + rank;
+        __builtin_amdgcn_wave_barrier();
+        if (has && rank == 0) mine[id] += (uint32_t)__builtin_popcountll(peers);
+        __builtin_amdgcn_wave_barrier();
+        if (i < s1) a.row_of[i] = has ? (int32_t)row : -1;
+        if (has) a.row_token[row] = (int32_t)(i / a.top_k);
+    }
+    // rows behind the last one
+    const uint32_t used = first[E], b0 = blockIdx.x * a.per_block, b1 = a.n - b0 < a.per_block ? a.n : b0 + a.per_block;
+    for (uint32_t r = b0 + tid; r < b1; r += threads)
+        if (r >= used) a.row_token[r] = -1;
+}
+
+// ---- moves: `lanes` threads (a power of two) for each token ----
+// Entries are taken kEntries at a time, so that their loads are under way together.
+constexpr int kEntries = 8;
+
+struct MoveShape {
+    uint32_t lanes, pieces;              // threads of a token, pieces of a row
+};
+
+template <int DT> __device__ __forceinline__ uint32_t entries_of(const MoveArgs &a, uint32_t t, uint32_t j0, uint32_t (&row)[kEntries]) {
+    const uint32_t n = a.top_k - j0 < (uint32_t)kEntries ? a.top_k - j0 : (uint32_t)kEntries, most = a.tokens * a.top_k;
+#pragma unroll
+    for (int j = 0; j < kEntries; ++j) {
+        row[j] = (uint32_t)j < n ? (uint32_t)a.row_of[(uint64_t)t * a.top_k + j0 + j] : ~0u;
+        if (row[j] >= most) row[j] = ~0u;
+    }
+    return n;
+}
+
+template <int DT> __global__ __launch_bounds__(256) void ft_expert_gather_kernel(MoveArgs a, MoveShape s) {
+    using T = RowType<DT>;
+    const uint32_t t = blockIdx.x * (256u / s.lanes) + threadIdx.x / s.lanes;
+    if (t >= a.tokens) return;
+    const unsigned char *const src = static_cast<const unsigned char *>(a.src) + (uint64_t)t * a.ld_token * T::BYTES;
+    unsigned char *const dst = static_cast<unsigned char *>(a.dst);
+    const uint64_t pitch = (uint64_t)a.ld_row * T::BYTES;
+    for (uint32_t j0 = 0; j0 < a.top_k; j0 += kEntries) {
+        uint32_t row[kEntries];
+        entries_of<DT>(a, t, j0, row);
+        for (uint32_t p = threadIdx.x & (s.lanes - 1u); p < s.pieces; p += s.lanes) {
+            const uint32_t n = a.cols - p * T::V;
+            const row_u32x4 v = T::load(src + p * 16u, n);
+#pragma unroll
+            for (int j = 0; j < kEntries; ++j)
+                if (row[j] != ~0u) T::store(dst + row[j] * pitch + p * 16u, v, n);
+        }
+    }
+}
+
+template <int DT> __global__ __launch_bounds__(256) void ft_expert_combine_kernel(MoveArgs a, MoveShape s) {
+    using T = RowType<DT>;
+    const uint32_t t = blockIdx.x * (256u / s.lanes) + threadIdx.x / s.lanes;
+    if (t >= a.tokens) return;
+    const unsigned char *const src = static_cast<const unsigned char *>(a.src);
+    unsigned char *const dst = static_cast<unsigned char *>(a.dst) + (uint64_t)t * a.ld_token * T::BYTES;
+    const uint64_t pitch = (uint64_t)a.ld_row * T::BYTES;
+    for (uint32_t p = threadIdx.x & (s.lanes - 1u); p < s.pieces; p += s.lanes) {
+        const uint32_t n = a.cols - p * T::V;
+        float sum[T::V] = {};
+        for (uint32_t j0 = 0; j0 < a.top_k; j0 += kEntries) {
+            uint32_t row[kEntries];
+            entries_of<DT>(a, t, j0, row);
+            row_u32x4 v[kEntries];
+            float w[kEntries];
+#pragma unroll
+            for (int j = 0; j < kEntries; ++j) {
+                v[j] = row_u32x4{0u, 0u, 0u, 0u};
+                w[j] = 1.f;
+                if (row[j] == ~0u) continue;
+                v[j] = T::load(src + row[j] * pitch + p * 16u, n);
+                if (a.weights) w[j] = a.weights[(uint64_t)t * a.top_k + j0 + j];
+            }
+#pragma unroll
+            for (int j = 0; j < kEntries; ++j) {
+                if (row[j] == ~0u) continue;
+                float f[T::V];
+                T::floats(v[j], f);
+#pragma unroll
+                for (int i = 0; i < T::V; ++i) sum[i] = __builtin_fmaf(w[j], f[i], sum[i]);
+            }
+        }
+        T::store(dst + p * 16u, T::pack(sum), n);
+    }
+}
+
+// dY and, where DW, dweights: each thread's share of the products dOut * Y in fp32, then over the token's threads
+template <int DT, bool DW> __global__ __launch_bounds__(256) void ft_expert_grad_kernel(MoveArgs a, MoveShape s) {
+    using T = RowType<DT>;
+    __shared__ float parts[4][kEntries];
+    const uint32_t t = blockIdx.x * (256u / s.lanes) + threadIdx.x / s.lanes, lane = threadIdx.x & 63u, wave = threadIdx.x / 64u;
+    const bool there = t < a.tokens;     // (a token's threads stay for the barriers where they are several waves)
+    const unsigned char *const dout = static_cast<const unsigned char *>(a.src) + (there ? (uint64_t)t * a.ld_token * T::BYTES : 0u);
+    const unsigned char *const y = static_cast<const unsigned char *>(a.other);
+    unsigned char *const dst = static_cast<unsigned char *>(a.dst);
+    const uint64_t pitch = (uint64_t)a.ld_row * T::BYTES;
+    for (uint32_t j0 = 0; j0 < a.top_k; j0 += kEntries) {
+        uint32_t row[kEntries];
+        float w[kEntries], dot[kEntries];
+        uint32_t n_entries = 0;
+#pragma unroll
+        for (int j = 0; j < kEntries; ++j) { row[j] = ~0u; w[j] = 1.f; dot[j] = 0.f; }
+        if (there) {
+            n_entries = entries_of<DT>(a, t, j0, row);
+            if (a.weights) {
+#pragma unroll
+                for (int j = 0; j < kEntries; ++j)
+                    if (row[j] != ~0u) w[j] = a.weights[(uint64_t)t * a.top_k + j0 + j];
+            }
+            for (uint32_t p = threadIdx.x & (s.lanes - 1u); p < s.pieces; p += s.lanes) {
+                const uint32_t n = a.cols - p * T::V;
+                float d[T::V];
+                T::floats(T::load(dout + p * 16u, n), d);
+                row_u32x4 v[kEntries];
+                if constexpr (DW) {
+#pragma unroll
+                    for (int j = 0; j < kEntries; ++j) {
+                        v[j] = row_u32x4{0u, 0u, 0u, 0u};
+                        if (row[j] != ~0u) v[j] = T::load(y + row[j] * pitch + p * 16u, n);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < kEntries; ++j) {
+                    if (row[j] == ~0u) continue;
+                    float g[T::V];
+#pragma unroll
+                    for (int i = 0; i < T::V; ++i) g[i] = w[j] * d[i];
+                    T::store(dst + row[j] * pitch + p * 16u, T::pack(g), n);
+                    if constexpr (DW) {
+                        float f[T::V];
+                        T::floats(v[j], f);
+#pragma unroll
+                        for (int i = 0; i < T::V; ++i) dot[j] = __builtin_fmaf(d[i], f[i], dot[j]);
+                    }
+                }
+            }
+        }
+        if constexpr (DW) {
+            const uint32_t in_wave = s.lanes < 64u ? s.lanes : 64u;
+#pragma unroll
+            for (int j = 0; j < kEntries; ++j)
+                for (uint32_t m = 1; m < in_wave; m *= 2) dot[j] += __shfl_xor(dot[j], (int)m);
+            if (s.lanes > 64u) {                             // (the same in every thread of the launch)
+                __syncthreads();
+                if (lane == 0) {
+#pragma unroll
+                    for (int j = 0; j < kEntries; ++j) parts[wave][j] = dot[j];
+                }
+                __syncthreads();
+                const uint32_t w0 = wave & ~(s.lanes / 64u - 1u);
+#pragma unroll
+                for (int j = 0; j < kEntries; ++j) {
+                    dot[j] = 0.f;
+                    for (uint32_t k = 0; k < s.lanes / 64u; ++k) dot[j] += parts[w0 + k][j];
+                }
+            }
+            if (there && (threadIdx.x & (s.lanes - 1u)) == 0) {
+#pragma unroll
+                for (int j = 0; j < kEntries; ++j)
+                    if ((uint32_t)j < n_entries) a.dweights[(uint64_t)t * a.top_k + j0 + j] = row[j] == ~0u ? 0.f : dot[j];
+            }
+        }
+    }
+}
+
+}  // namespace ftk
+
+using namespace ftk;
+
+namespace {
+
+template <int DT> MoveShape move_shape(const MoveArgs &a) {
+    MoveShape s;
+    s.pieces = (a.cols + RowType<DT>::V - 1) / RowType<DT>::V;
+    s.lanes = 8;
+    while (s.lanes < 256u && s.lanes < s.pieces) s.lanes *= 2u;
+    return s;
+}
+enum { MOVE_GATHER, MOVE_COMBINE, MOVE_GRAD };
+template <int DT> void move_launch(int what, const MoveArgs &a, hipStream_t stream) {
+    const MoveShape s = move_shape<DT>(a);
+    const uint32_t per = 256u / s.lanes;
+    const dim3 grid((uint32_t)(((uint64_t)a.tokens + per - 1u) / per)), block(256);
+    if (what == MOVE_GATHER) hipLaunchKernelGGL((ft_expert_gather_kernel<DT>), grid, block, 0, stream, a, s);
+    else if (what == MOVE_COMBINE) hipLaunchKernelGGL((ft_expert_combine_kernel<DT>), grid, block, 0, stream, a, s);
+    else if (a.dweights) hipLaunchKernelGGL((ft_expert_grad_kernel<DT, true>), grid, block, 0, stream, a, s);
+    else hipLaunchKernelGGL((ft_expert_grad_kernel<DT, false>), grid, block, 0, stream, a, s);
+}
+ft_status move(int what, const ft_expert_desc *desc, const MoveArgs &a, void *stream) {
+    const ft_status st = op_stream_check(stream);
+    if (st != FT_OK) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (desc->dtype == FT_F16) move_launch<ROW_F16>(what, a, s);
+    else if (desc->dtype == FT_BF16) move_launch<ROW_BF16>(what, a, s);
+    else move_launch<ROW_F32>(what, a, s);
+    return op_launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+ft_status ft_expert_workspace(const ft_expert_desc *desc, uint32_t tokens, uint64_t *bytes) { return expert_workspace(desc, tokens, bytes); }
+
+ft_status ft_expert_sort(const ft_expert_desc *desc, uint32_t tokens, const int32_t *expert_of, int32_t *offsets, int32_t *row_token, int32_t *row_of, void *workspace,
+                         uint64_t workspace_bytes, void *hip_stream) {
+    ft_status st = sort_check(desc, tokens, expert_of, offsets, row_token, row_of, workspace, workspace_bytes);
+    if (st == FT_OK) st = op_stream_check(hip_stream);
+    if (st != FT_OK) return st;
+    SortArgs a = {};
+    a.ids = expert_of; a.offsets = offsets; a.row_token = row_token; a.row_of = row_of;
+    a.counts = static_cast<uint32_t *>(workspace);
+    a.n = tokens * desc->top_k; a.experts = desc->experts; a.top_k = desc->top_k;
+    a.blocks = sort_blocks(a.n);
+    a.per_block = a.blocks == 1u ? (a.n ? a.n : 1u) : (uint32_t)(((uint64_t)a.n + a.blocks - 1u) / a.blocks + 63u) / 64u * 64u;
+    a.blocks = a.n ? (a.n + a.per_block - 1u) / a.per_block : 1u;
+    while (a.id_bits < 10u && (1u << a.id_bits) < a.experts) ++a.id_bits;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    uint32_t waves = (uint32_t)(((uint64_t)a.per_block + 63u) / 64u);
+    if (waves > 16u) waves = 16u;
+    while (waves > 1u && (waves * a.experts + 2u * a.experts + 1u) * 4u > 65536u) --waves;         // (what a kernel may have without a raised limit)
+    if (a.blocks > 1u) {
+        hipLaunchKernelGGL(ft_expert_count, dim3(a.blocks), dim3(1024), a.experts * 4u, s, a);
+        st = op_launched();
+        if (st != FT_OK) return st;
+    }
+    hipLaunchKernelGGL(ft_expert_place, dim3(a.blocks), dim3(waves * 64u), (waves * a.experts + 2u * a.experts + 1u) * 4u, s, a);
+    return op_launched();
+}
+
+ft_status ft_expert_gather(const ft_expert_desc *desc, uint32_t tokens, const void *X, const int32_t *row_of, void *Y, void *hip_stream) {
+    MoveArgs a = {};
+    a.src = X; a.dst = Y; a.row_of = row_of;
+    bool launch;
+    const ft_status st = move_check(desc, tokens, false, &a, &launch);
+    return st != FT_OK || !launch ? st : move(MOVE_GATHER, desc, a, hip_stream);
+}
+
+ft_status ft_expert_combine(const ft_expert_desc *desc, uint32_t tokens, const void *Y, const int32_t *row_of, const float *weights, void *Out, void *hip_stream) {
+    MoveArgs a = {};
+    a.src = Y; a.dst = Out; a.row_of = row_of; a.weights = weights;
+    bool launch;
+    const ft_status st = move_check(desc, tokens, false, &a, &launch);
+    return st != FT_OK || !launch ? st : move(MOVE_COMBINE, desc, a, hip_stream);
+}
+
+ft_status ft_expert_combine_grad(const ft_expert_desc *desc, uint32_t tokens, const void *dOut, const void *Y, const int32_t *row_of, const float *weights, void *dY,
+                                 float *dweights, void *hip_stream) {
+    MoveArgs a = {};
+    a.src = dOut; a.other = Y; a.dst = dY; a.row_of = row_of; a.weights = weights; a.dweights = dweights;
+    bool launch;
+    const ft_status st = move_check(desc, tokens, dweights != nullptr, &a, &launch);
+    return st != FT_OK || !launch ? st : move(MOVE_GRAD, desc, a, hip_stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,201 @@
+// Rows of values as 8-bit integers with one scale each, where asked after silu(gate) * up.
+//
+// Bound by memory: a row is read once, stays in its threads' registers while its largest magnitude is found, and
+// leaves as integers.  Rows of more than 32768 columns are read a second time.
+//
+// scale = amax / 127 and q = 127 f / amax to nearest even.  For 16-bit f this is exact without a division for each value: t = f *
+// (127 / amax) is off by at most 2^-23 of itself.  127 f / amax lies exactly in the middle between two integers or at
+// least 2^-19 of itself away from there (f = a 2^p, amax = d 2^q with a, d < 2^11 make 254 a 2^p - odd d 2^q a multiple of 2^p, and
+// 2^p / (2 d 2^q) over 127 a 2^p / (d 2^q) is more than 2^-19).  So t rounded to 21 bits -- the middles have at most 9 -- rounds
+// to the integer that the exact quotient rounds to.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "ft_internal.h"
+#include "i8_ops.h"
+#include "lane_types.h"
+#include "op_launch.h"
+
+namespace ftk {
+
+// t to 21 bits (Veltkamp's splitting; t <= 127)
+__device__ __forceinline__ float to_21_bits(float t) {
+#pragma clang fp contract(off)
+    const float c = t * 9.f;
+    const float d = c - t;
+    return c - d;
+}
+
+// The values of a piece of 8 columns, zeros beyond the row's end
+template <int DT, bool GATED> struct QuantPiece {
+    using T = RowType<DT>;
+    static constexpr int N = 8 / T::V;                       // loads of 16 bytes
+    struct Raw { row_u32x4 x[N], up[GATED ? N : 1]; };
+    static __device__ __forceinline__ void eight(const row_u32x4 (&x)[N], float (&f)[8]) {
+#pragma unroll
+        for (int h = 0; h < N; ++h) {
+            float part[T::V];
+            T::floats(x[h], part);
+#pragma unroll
+            for (int i = 0; i < T::V; ++i) f[h * T::V + i] = part[i];
+        }
+    }
+    static __device__ __forceinline__ void values(const Raw &r, float (&f)[8]) {
+        eight(r.x, f);
+        if constexpr (GATED) {
+            float u[8];
+            eight(r.up, u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = silu_mul(f[i], u[i]);
+        }
+    }
+    static __device__ __forceinline__ void clear(Raw &r) {
+#pragma unroll
+        for (int h = 0; h < N; ++h) {
+            r.x[h] = row_u32x4{0u, 0u, 0u, 0u};
+            if constexpr (GATED) r.up[h] = row_u32x4{0u, 0u, 0u, 0u};
+        }
+    }
+    static __device__ __forceinline__ void load(const QuantArgs &a, const unsigned char *row, uint32_t p, Raw &r) {
+        clear(r);
+        const uint32_t n = a.cols - p * 8u;
+#pragma unroll
+        for (int h = 0; h < N; ++h) {
+            if (h && n <= (uint32_t)(h * T::V)) continue;
+            r.x[h] = T::load(row + p * (8u * T::BYTES) + h * 16u, n - h * T::V);
+            if constexpr (GATED) r.up[h] = T::load(row + (a.cols + p * 8u) * T::BYTES + h * 16u, n - h * T::V);
+        }
+    }
+};
+
+// Largest magnitude as bits: magnitudes compare as their bits do, infinities and NaNs above all others
+__device__ __forceinline__ uint32_t largest(const float (&f)[8], uint32_t m) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t b = __builtin_bit_cast(uint32_t, f[i]) & 0x7fffffffu;
+        m = b > m ? b : m;
+    }
+    return m;
+}
+
+struct RowScale {
+    float up, per;                       // q = f * up * per; rows of tiny values are lifted so that 127 / amax is finite
+    float scale;
+};
+__device__ __forceinline__ RowScale row_scale(uint32_t bits) {
+    RowScale r = {1.f, 0.f, 0.f};
+    if (bits >= 0x7f800000u) r.scale = __builtin_nanf("");
+    else if (bits != 0) {
+        const float amax = __builtin_bit_cast(float, bits);
+        if (amax < 0x1p-100f) r.up = 0x1p100f;
+        r.per = 127.f / (amax * r.up);
+        r.scale = amax / 127.f;
+    }
+    return r;
+}
+__device__ __forceinline__ uint2 integers(const float (&f)[8], const RowScale &r, bool fine) {
+    uint32_t w[2] = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int q = fine ? (int)__builtin_rintf(to_21_bits(f[i] * r.up * r.per)) : 0;
+        w[i / 4] |= ((uint32_t)q & 255u) << (i % 4 * 8);
+    }
+    return make_uint2(w[0], w[1]);
+}
+
+// `threads` threads for a row: 64, four rows to a workgroup, or a whole workgroup.  HELD: pieces that a thread keeps; 0: as many as
+// there are, read twice
+template <int DT, bool GATED, int HELD> __global__ __launch_bounds__(1024) void ft_quant(QuantArgs a, uint32_t threads) {
+    using P = QuantPiece<DT, GATED>;
+    __shared__ uint32_t most[16];
+    const uint32_t per = threads == 64u ? blockDim.x / 64u : 1u;
+    const uint32_t r = blockIdx.x * per + (per > 1u ? threadIdx.x / 64u : 0u), tid = per > 1u ? threadIdx.x & 63u : threadIdx.x;
+    if (per > 1u && r >= a.rows) return;                     // (whole waves, and no barrier below for them)
+    const unsigned char *const row = static_cast<const unsigned char *>(a.X) + (uint64_t)r * a.ldx * P::T::BYTES;
+    unsigned char *const out = reinterpret_cast<unsigned char *>(a.Q) + (uint64_t)r * a.ldq;
+    const uint32_t pieces = (a.cols + 7u) / 8u;
+    constexpr int H = HELD ? HELD : 1;
+    float f[H][8];
+    uint32_t m = 0;
+    if constexpr (HELD > 0) {
+        typename P::Raw x[H];
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+            if (tid + i * threads < pieces) P::load(a, row, tid + i * threads, x[i]);
+            else P::clear(x[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+            P::values(x[i], f[i]);
+            m = largest(f[i], m);
+        }
+    } else {
+        for (uint32_t p = tid; p < pieces; p += threads) {
+            typename P::Raw x;
+            P::load(a, row, p, x);
+            P::values(x, f[0]);
+            m = largest(f[0], m);
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t o = __shfl_xor(m, d);
+        m = o > m ? o : m;
+    }
+    if (threads > 64u) {
+        if ((threadIdx.x & 63u) == 0) most[threadIdx.x / 64u] = m;
+        __syncthreads();
+        for (uint32_t w = 0; w < threads / 64u; ++w) m = most[w] > m ? most[w] : m;
+    }
+    const bool fine = m < 0x7f800000u;
+    const RowScale s = row_scale(m);
+    if (tid == 0) a.scale[r] = s.scale;
+    if constexpr (HELD > 0) {
+#pragma unroll
+        for (int i = 0; i < H; ++i)
+            if (tid + i * threads < pieces) *reinterpret_cast<uint2 *>(out + (tid + i * threads) * 8u) = integers(f[i], s, fine);
+    } else {
+        for (uint32_t p = tid; p < pieces; p += threads) {
+            typename P::Raw x;
+            P::load(a, row, p, x);
+            P::values(x, f[0]);
+            *reinterpret_cast<uint2 *>(out + p * 8u) = integers(f[0], s, fine);
+        }
+    }
+    for (uint32_t p = pieces + tid; p < a.ldq / 8u; p += threads) *reinterpret_cast<uint2 *>(out + p * 8u) = make_uint2(0u, 0u);
+}
+
+}  // namespace ftk
+
+using namespace ftk;
+
+namespace {
+
+template <int DT, bool GATED> void launch(const QuantArgs &a, hipStream_t s) {
+    // two pieces a thread where the row has that many
+    const uint32_t pieces = (a.cols + 7u) / 8u;
+    uint32_t threads = ((pieces + 1u) / 2u + 63u) / 64u * 64u;
+    if (threads > 1024u) threads = 1024u;
+    const uint32_t per = threads == 64u ? 4u : 1u;
+    const dim3 grid((a.rows + per - 1u) / per), block(threads * per);
+    if (pieces <= threads) hipLaunchKernelGGL((ft_quant<DT, GATED, 1>), grid, block, 0, s, a, threads);
+    else if (pieces <= 2u * threads) hipLaunchKernelGGL((ft_quant<DT, GATED, 2>), grid, block, 0, s, a, threads);
+    else if (pieces <= 4u * threads) hipLaunchKernelGGL((ft_quant<DT, GATED, 4>), grid, block, 0, s, a, threads);
+    else hipLaunchKernelGGL((ft_quant<DT, GATED, 0>), grid, block, 0, s, a, threads);
+}
+
+}  // namespace
+
+extern "C" ft_status ft_i8_quantize(const ft_quant_desc *desc, uint32_t rows, const void *X, int8_t *Q, float *scale, void *hip_stream) {
+    QuantArgs a = {};
+    bool go;
+    ft_status st = quant_check(desc, rows, X, Q, scale, &a, &go);
+    if (st == FT_OK && go) st = op_stream_check(hip_stream);
+    if (st != FT_OK || !go) return st;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    const bool gated = desc->act == FT_ACT_SILU_MUL;
+    if (desc->dtype == FT_F16) gated ? launch<ROW_F16, true>(a, s) : launch<ROW_F16, false>(a, s);
+    else if (desc->dtype == FT_BF16) gated ? launch<ROW_BF16, true>(a, s) : launch<ROW_BF16, false>(a, s);
+    else gated ? launch<ROW_F32, true>(a, s) : launch<ROW_F32, false>(a, s);
+    return op_launched();
+}

@@ -1,0 +1,191 @@
+"""The operators together, as a program uses them: a feed-forward layer of experts served in 8 bits, alone and in a captured graph, and a
+training step of such a layer in 16 bits, whose products are grouped launches."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2407_21418_amd as ft
+
+from gpu_util import stream
+from test_gpu_experts import route
+from test_gpu_i8_products import gated
+
+pytestmark = pytest.mark.gpu
+
+
+def pitch(k):
+    return (k + 15) // 16 * 16
+
+
+class Layer:
+    """silu(x W1g) * (x W1u), W2, weighted sum over each token's experts."""
+
+    def __init__(self, tokens, top_k, experts, cols, ffn, seed=0):
+        g = self.gen = torch.Generator(device="cuda").manual_seed(seed)
+        self.tokens, self.top_k, self.experts, self.cols, self.ffn, self.rows = tokens, top_k, experts, cols, ffn, tokens * top_k
+        weight = lambda n, k: (torch.randint(-127, 128, (n, pitch(k)), generator=g, device="cuda", dtype=torch.int8),  # noqa: E731
+                               (torch.rand(n, generator=g, device="cuda") + 0.5) / (73 * k ** 0.5))
+        (self.w1, self.s1), (self.w2, self.s2) = weight(experts * 2 * ffn, cols), weight(experts * cols, ffn)
+        i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")  # noqa: E731
+        self.ids, self.offsets, self.row_token, self.row_of = i32(tokens, top_k), i32(experts + 1), i32(self.rows), i32(self.rows)
+        self.weights = torch.zeros(tokens, top_k, device="cuda")
+        half = dict(dtype=torch.bfloat16, device="cuda")
+        self.x, self.out = torch.zeros(tokens, cols, **half), torch.zeros(tokens, cols, **half)
+        self.h, self.y = torch.zeros(self.rows, ffn, device="cuda"), torch.zeros(self.rows, cols, **half)
+        self.q, self.sx = torch.zeros(tokens, pitch(cols), dtype=torch.int8, device="cuda"), torch.zeros(tokens, device="cuda")
+        self.qh, self.sh = torch.zeros(self.rows, pitch(ffn), dtype=torch.int8, device="cuda"), torch.zeros(self.rows, device="cuda")
+        self.route = ft.ft_expert_desc(experts=experts, top_k=top_k, cols=cols, dtype=ft.FT_BF16)
+        self.workspace = torch.zeros(max(16, ft.ft_expert_workspace(self.route, tokens)), dtype=torch.uint8, device="cuda")
+        self.quant_x, self.quant_h = ft.ft_quant_desc(cols=cols, dtype=ft.FT_BF16), ft.ft_quant_desc(cols=ffn, dtype=ft.FT_F32)
+        self.up = ft.ft_i8_desc(n=2 * ffn, k=cols, epilogue=ft.FT_EPI_SILU_MUL, experts=experts)
+        self.down = ft.ft_i8_desc(n=cols, k=ffn, dtype=ft.FT_BF16, out_dtype=ft.FT_OUT_SAME, experts=experts)
+        self.refill(seed, 0)
+
+    def refill(self, seed, padded):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.x.copy_(torch.randn(self.tokens, self.cols, generator=g, device="cuda"))
+        values, ids = torch.topk(torch.randn(self.tokens, self.experts, generator=g, device="cuda"), self.top_k, dim=1)
+        self.ids.copy_(ids)
+        self.ids[self.tokens - padded:] = -1
+        self.weights.copy_(torch.softmax(values, dim=1))
+
+    def run(self):
+        s, p = stream(), lambda t: t.data_ptr()  # noqa: E731
+        ft.ft_expert_sort(self.route, self.tokens, p(self.ids), p(self.offsets), p(self.row_token), p(self.row_of), p(self.workspace), self.workspace.numel(), s)
+        ft.ft_i8_quantize(self.quant_x, self.tokens, p(self.x), p(self.q), p(self.sx), s)
+        ft.ft_i8_matmul_experts(self.up, self.rows, p(self.offsets), p(self.q), p(self.sx), p(self.row_token), self.tokens, p(self.w1), p(self.s1), 0, p(self.h), s)
+        ft.ft_i8_quantize(self.quant_h, self.rows, p(self.h), p(self.qh), p(self.sh), s)
+        ft.ft_i8_matmul_experts(self.down, self.rows, p(self.offsets), p(self.qh), p(self.sh), 0, self.rows, p(self.w2), p(self.s2), 0, p(self.y), s)
+        ft.ft_expert_combine(self.route, self.tokens, p(self.y), p(self.row_of), p(self.weights), p(self.out), s)
+
+    def check(self):
+        """Every stage against 64 bits of what the stage before it left: the products to four roundings in fp32 and one to bf16, the
+        activations to what test_gpu_i8_products says of them, their integers to half a step and what fp32 leaves open (see
+        test_gpu_quant_rows), the sums to top_k roundings."""
+        torch.cuda.synchronize()
+        offsets, row_token, row_of = route(self.ids.cpu().numpy(), self.experts)
+        assert np.array_equal(self.offsets.cpu().numpy(), offsets) and np.array_equal(self.row_token.cpu().numpy(), row_token) and np.array_equal(self.row_of.cpu().numpy(), row_of)
+        f = self.x.double()
+        peak = f.abs().amax(1, keepdim=True)
+        assert torch.equal(self.q[:, :self.cols].double(), torch.round(127 * f / peak)) and torch.equal(self.sx, (peak[:, 0] / 127).float())
+
+        def product(q, s, w, sw, n, k, e):
+            return (q[:, :k].double() @ w[e * n:(e + 1) * n, :k].double().t()) * s.double()[:, None] * sw[e * n:(e + 1) * n].double()
+
+        token = torch.from_numpy(row_token).cuda()
+        for e in range(self.experts):
+            rows = slice(int(offsets[e]), int(offsets[e + 1]))
+            if rows.start == rows.stop:
+                continue
+            p = product(self.q[token[rows]], self.sx[token[rows]], self.w1, self.s1, 2 * self.ffn, self.cols, e)
+            f, bound = gated(p)
+            assert bool(((self.h[rows].double() - f).abs() <= bound).all())
+            f = self.h[rows].double()
+            peak = f.abs().amax(1, keepdim=True)
+            assert bool(((self.qh[rows, :self.ffn].double() - 127 * f / peak).abs() <= 0.5 + 127 * 3.5 * 2.0 ** -23).all())
+            assert torch.equal(self.sh[rows], (peak[:, 0] / 127).float())
+            ref = product(self.qh[rows], self.sh[rows], self.w2, self.s2, self.cols, self.ffn, e)
+            assert bool(((self.y[rows].double() - ref).abs() <= (2.0 ** -8 * 1.0001 + 4.01 * 2.0 ** -24) * ref.abs() + 2.0 ** -134).all())
+        at = torch.from_numpy(row_of).cuda()
+        terms = torch.where((at >= 0)[:, None], self.y[at.clamp(min=0)].double(), torch.zeros((), dtype=torch.float64, device="cuda")).reshape(self.tokens, self.top_k, self.cols)
+        terms = terms * self.weights.double()[:, :, None]
+        ref = terms.sum(dim=1)
+        assert bool(((self.out.double() - ref).abs() <= self.top_k * 2.0 ** -24 * terms.abs().sum(dim=1) * 1.0001 + 2.0 ** -8 * 1.0001 * ref.abs() + 2.0 ** -134).all())
+
+
+@pytest.mark.parametrize("tokens,top_k,experts,cols,ffn,padded", [(1, 2, 4, 64, 48, 0), (4, 2, 8, 1024, 1408, 0), (64, 4, 64, 512, 704, 3), (1000, 2, 16, 1000, 715, 37), (777, 3, 5, 256, 320, 777), (3000, 4, 6, 640, 512, 0)])
+def test_layer_in_8_bits(tokens, top_k, experts, cols, ffn, padded):
+    layer = Layer(tokens, top_k, experts, cols, ffn)
+    layer.refill(5, padded)
+    layer.run()
+    layer.check()
+
+
+def test_layers_in_captured_graphs():
+    """Two graphs that share a workspace, replayed in turn with other tokens each time."""
+    a, b = Layer(300, 4, 16, 256, 320), Layer(5000, 4, 16, 128, 64, seed=1)
+    a.workspace = b.workspace
+    graphs = []
+    for layer in (a, b):
+        layer.run()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            layer.run()
+        graphs.append(g)
+    for turn in range(3):
+        for layer, g in zip((a, b), graphs):
+            layer.refill(100 + turn, 10 * turn)
+            layer.out.fill_(float("nan"))
+            g.replay()
+            layer.check()
+            captured = layer.out.clone()
+            layer.out.fill_(float("nan"))
+            layer.run()
+            torch.cuda.synchronize()
+            assert torch.equal(layer.out, captured)
+
+
+def test_layers_on_two_streams_at_once():
+    layers = [Layer(700, 3, 8, 256, 192, seed=s) for s in (1, 2)]
+    streams = [torch.cuda.Stream() for _ in layers]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for layer, s in zip(layers, streams):
+            with torch.cuda.stream(s):
+                layer.run()
+    for layer in layers:
+        layer.check()
+
+
+def test_training_step_in_16_bits():
+    """Router weights w, tokens x and the experts' weights: forward and backward through sort, gather, grouped Matmuls, combine and their
+    gradients, against torch's gradients in 64 bits of the same 16-bit values.  Every stage rounds to fp16 once (2^-11) and a gradient passes three
+    of them, each a sum of values that were rounded alone: norms agree to 4 * 2^-11."""
+    tokens, top_k, experts, cols, out_cols = 200, 2, 6, 128, 96
+    g = torch.Generator().manual_seed(11)
+    x = torch.randn(tokens, cols, generator=g).half()
+    W = (torch.randn(experts, cols, out_cols, generator=g) / cols ** 0.5).half()
+    dout = torch.randn(tokens, out_cols, generator=g).half()
+    ids = torch.stack([torch.randperm(experts, generator=g)[:top_k] for _ in range(tokens)]).int()
+    ids[-9:] = -1
+    w = torch.rand(tokens, top_k, generator=g)
+    # 64 bits
+    x64, W64, w64 = x.double().requires_grad_(), W.double().requires_grad_(), w.double().requires_grad_()
+    ref = torch.zeros(tokens, out_cols, dtype=torch.float64)
+    for e in range(experts):
+        t, j = torch.nonzero(ids == e, as_tuple=True)
+        ref = ref.index_add(0, t, (x64[t] @ W64[e]) * w64[t, j][:, None])
+    (ref * dout.double()).sum().backward()
+    # the framework
+    n, s = tokens * top_k, stream()
+    dev = lambda t: t.cuda().contiguous()  # noqa: E731
+    zeros = lambda *shape, dtype=torch.float16: torch.zeros(shape, dtype=dtype, device="cuda")  # noqa: E731
+    xd, Wd, wd, dd, idd = dev(x), dev(W), dev(w), dev(dout), dev(ids)
+    into, out_of = ft.ft_expert_desc(experts=experts, top_k=top_k, cols=cols), ft.ft_expert_desc(experts=experts, top_k=top_k, cols=out_cols)
+    offsets, row_token, row_of = (zeros(k, dtype=torch.int32) for k in (experts + 1, n, n))
+    ws = zeros(max(16, ft.ft_expert_workspace(into, tokens)), dtype=torch.uint8)
+    ft.ft_expert_sort(into, tokens, idd.data_ptr(), offsets.data_ptr(), row_token.data_ptr(), row_of.data_ptr(), ws.data_ptr(), ws.numel(), s)
+    xs, ys, out = zeros(n, cols), zeros(n, out_cols), zeros(tokens, out_cols)
+    ft.ft_expert_gather(into, tokens, xd.data_ptr(), row_of.data_ptr(), xs.data_ptr(), s)
+    sizes = np.diff(offsets.cpu().numpy()).tolist()
+
+    def products(shapes, A, B, C, **desc):
+        op = ft.ft_op_register(ft.ft_op_desc(kind=ft.FT_OP_BMM, dtype=ft.FT_F16, out_dtype=ft.FT_OUT_SAME, batch_hi=experts, **desc))
+        plan = ft.ft_plan_create_grouped(op, ft.ft_ukernels_derive(op), shapes)
+        ft.ft_launch(plan, A.data_ptr(), B.data_ptr(), C.data_ptr(), s)
+        torch.cuda.synchronize()
+
+    products([ft.ft_shape(batch=1, m=c) for c in sizes], xs, Wd, ys, n=out_cols, k=cols, m_lo=0, m_hi=n)
+    ft.ft_expert_combine(out_of, tokens, ys.data_ptr(), row_of.data_ptr(), wd.data_ptr(), out.data_ptr(), s)
+    dys, dw, dxs, dx, dW = zeros(n, out_cols), zeros(tokens, top_k, dtype=torch.float32), zeros(n, cols), zeros(tokens, cols), zeros(experts, cols, out_cols)
+    ft.ft_expert_combine_grad(out_of, tokens, dd.data_ptr(), ys.data_ptr(), row_of.data_ptr(), wd.data_ptr(), dys.data_ptr(), dw.data_ptr(), s)
+    products([ft.ft_shape(batch=1, m=c) for c in sizes], dys, Wd, dxs, n=cols, k=out_cols, m_lo=0, m_hi=n, b_layout=ft.FT_B_NK)
+    xt = torch.cat([xs[a:a + c].t().reshape(-1) for a, c in zip(offsets.tolist(), sizes)])
+    products([ft.ft_shape(batch=1, k=c) for c in sizes], xt, dys, dW, m=cols, n=out_cols, k_lo=0, k_hi=n)
+    ft.ft_expert_combine(into, tokens, dxs.data_ptr(), row_of.data_ptr(), 0, dx.data_ptr(), s)
+    torch.cuda.synchronize()
+    for got, want in ((out, ref.detach()), (dx, x64.grad), (dW, W64.grad), (dw, w64.grad)):
+        off = float((got.double().cpu() - want).norm() / want.norm())
+        assert off <= 4 * 2.0 ** -11, off
+    assert bool((dx[-9:] == 0).all()) and bool((dw[-9:] == 0).all()) and bool((out[-9:] == 0).all())
