@@ -13,6 +13,7 @@
 #include "ft_internal.h"
 #include "i8_ops.h"
 #include "lane_types.h"
+#include "lds_limit.h"
 #include "op_launch.h"
 
 namespace ftk {
@@ -60,7 +61,7 @@ __device__ __forceinline__ void stretch_of(const SortArgs &a, uint32_t wave, uin
 
 // counts[block][expert] of more than one block
 __global__ __launch_bounds__(1024) void ft_expert_count(SortArgs a) {
-    extern __shared__ uint32_t lds[];
+    __shared__ uint32_t lds[kMaxExperts];
     const uint32_t tid = threadIdx.x, threads = blockDim.x;
     for (uint32_t e = tid; e < a.experts; e += threads) lds[e] = 0u;
     __syncthreads();
@@ -348,9 +349,10 @@ ft_status ft_expert_sort(const ft_expert_desc *desc, uint32_t tokens, const int3
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     uint32_t waves = (uint32_t)(((uint64_t)a.per_block + 63u) / 64u);
     if (waves > 16u) waves = 16u;
-    while (waves > 1u && (waves * a.experts + 2u * a.experts + 1u) * 4u > 65536u) --waves;         // (what a kernel may have without a raised limit)
+    const hipError_t e = raise_lds_limit<&ft_expert_place>();
+    if (e != hipSuccess) { ftd_set_hip_error((int)e); return FT_ERR_HIP; }
     if (a.blocks > 1u) {
-        hipLaunchKernelGGL(ft_expert_count, dim3(a.blocks), dim3(1024), a.experts * 4u, s, a);
+        hipLaunchKernelGGL(ft_expert_count, dim3(a.blocks), dim3(1024), 0, s, a);
         st = op_launched();
         if (st != FT_OK) return st;
     }

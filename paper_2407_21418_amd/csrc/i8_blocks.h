@@ -1,0 +1,71 @@
+// Matmuls in 8-bit integers: which kernel a launch takes, and its grid.
+#pragma once
+#include "i8_ops.h"
+
+namespace ftk {
+
+// I8_STREAM: tiles of 16 x 16 (16 x 32 with gates) straight from memory into the matrix cores (i8_gemm.hip); the others pass through LDS
+// (i8_blocks.hip), I8_64x64 with two groups of waves along the reduce axis.
+enum I8Kind { I8_STREAM, I8_64x64, I8_64x128, I8_128x128, I8_128x256, I8_256x256, I8_KINDS };
+
+struct I8KindInfo {
+    uint32_t tm, tn, per_cu;             // tile, workgroups that a CU holds
+    // microseconds of a launch: once, for each round of tiles, for each k-tile of 128 of a round; for all tiles that there are over
+    // those of a round, and for each k-tile of theirs.  The first kind of a round's cost is latency, which is there however
+    // few its tiles are; the second is what they share: the caches' bandwidth and the power.
+    float once, round, round_k, tile, tile_k;
+};
+// Least squares over 204 shapes, m 8 .. 4096, n 768 .. 11008, k 768 .. 4096, all kinds measured at each (bf16 results, an idle device): the times
+// are met to 3 .. 9 % (root of the mean square), and the kind with the least is within 0.5 % of the fastest on average, 6 % at most.
+constexpr I8KindInfo kI8Kinds[I8_KINDS] = {
+    {16, 16, 1, 2.85f, 0.43f, 0.096f, 0.17f, 0.012f},
+    {64, 64, 1, 2.88f, 0.92f, 0.153f, 1.02f, 0.028f},
+    {64, 128, 2, 3.69f, 0.46f, 0.240f, 1.93f, 0.249f},
+    {128, 128, 2, 3.99f, 0.00f, 0.459f, 3.61f, 0.388f},
+    {128, 256, 1, 3.59f, 2.10f, 0.539f, 2.85f, 0.159f},
+    {256, 256, 1, 3.96f, 3.85f, 0.949f, 5.16f, 0.193f},
+};
+inline I8KindInfo i8_kind_info(I8Kind kind, bool gated) {
+    I8KindInfo i = kI8Kinds[kind];
+    if (kind == I8_STREAM && gated) i.tn = 32;
+    return i;
+}
+
+// Rows of tiles, about, where experts have different numbers of rows: each that has any ends in a tile that is half full on average.
+inline float i8_row_tiles(const I8Args &a, uint32_t tm, bool grouped) {
+    if (!grouped) return (float)((a.m + tm - 1u) / tm);
+    const float used = (float)(a.experts < a.m ? a.experts : a.m), full = (float)a.m / (float)tm + 0.5f * used;
+    return full > used ? full : used;
+}
+inline float i8_time(const I8Args &a, I8Kind kind, bool grouped) {
+    const I8KindInfo i = i8_kind_info(kind, a.gated != 0);
+    const float tiles = i8_row_tiles(a, i.tm, grouped) * (float)((a.n + i.tn - 1u) / i.tn), share = tiles / (float)(a.cus * i.per_cu), k = (float)((a.k + 127u) / 128u);
+    float rounds = (float)(uint32_t)share;
+    if (rounds < share) rounds += 1.f;
+    return i.once + rounds * (i.round + i.round_k * k) + share * (i.tile + i.tile_k * k);
+}
+inline I8Kind i8_choose(const I8Args &a, bool grouped) {
+    I8Kind best = I8_STREAM;
+    float least = i8_time(a, best, grouped);
+    for (int k = 1; k < I8_KINDS; ++k) {
+        const float t = i8_time(a, (I8Kind)k, grouped);
+        if (t < least) { least = t; best = (I8Kind)k; }
+    }
+    return best;
+}
+
+// The grid of a launch in tiles of tm x tn; false: more workgroups than a launch has.  By expert the rows of tiles are the most there can
+// be: all tiles full but the last of each expert.
+inline bool i8_grid(I8Args &a, uint32_t tm, uint32_t tn, bool grouped) {
+    const uint64_t rows = grouped ? (uint64_t)a.m / tm + (a.experts < a.m ? a.experts : a.m) : ((uint64_t)a.m + tm - 1) / tm;
+    a.col_tiles = (a.n + tn - 1) / tn;
+    if (rows * a.col_tiles > 0x7fffffffull) return false;
+    a.row_tiles = (uint32_t)rows;
+    const uint32_t band = tm >= 256 ? 4u : tm >= 128 ? 8u : 16u;       // rows of tiles that are walked together
+    a.group = a.row_tiles < band ? a.row_tiles : band;
+    return true;
+}
+
+ft_status i8_launch_blocks(I8Kind kind, bool grouped, I8Args &a, void *stream);
+
+}  // namespace ftk

@@ -1,0 +1,357 @@
+// Matmuls in 8-bit integers in blocks that pass through LDS: products of many rows.
+//
+// The loop is that of the large 16-bit products (big_gemm.hip), for the same bytes and twice the products: k-tiles of 128 bytes,
+// the fragments of one k-step of 64 in registers while the MFMAs of the other run, one barrier for each k-tile half-way
+// through its MFMAs, copies straight into LDS spread between them.  Both operands lie with k contiguous, so both are read with
+// ds_read_b128; chunks of 16 bytes are swizzled by their row.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "ft_internal.h"
+#include "i8_blocks.h"
+#include "i8_tile.h"
+#include "lds_limit.h"
+#include "op_launch.h"
+
+namespace ftk {
+
+template <int OFF> __device__ __forceinline__ i8_u32x4 i8_read(uint32_t addr) {
+    i8_u32x4 v;
+    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
+    return v;
+}
+template <int N> __device__ __forceinline__ void i8_wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void i8_copy(__amdgpu_buffer_rsrc_t r, unsigned char *lds_wave_base, uint32_t lane_off, uint32_t tile_off) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)lds_wave_base, 16, (int)lane_off, (int)tile_off, 0, 0);
+}
+// sixteen rows read at four neighbouring chunks: no bank conflicts (counted)
+__device__ __forceinline__ uint32_t i8_swizzle(uint32_t row) { return row & 7u; }
+template <int Q, int E, typename F> __device__ __forceinline__ void i8_each(F f) {
+    if constexpr (Q < E) { f(std::integral_constant<int, Q>{}); i8_each<Q + 1, E>(f); }
+}
+
+// A block of GM * WM rows by GN * WN columns.  STAGES = 0: A and B tiles are equally large and take turns in five slots (tile t: A in slot
+// 2t mod 5, B in slot (2t + 1) mod 5).  Otherwise a ring of STAGES stages of A and B.  GK = 2: two groups of GM * GN waves take every other
+// k-tile, each through a ring of its own, and share out the rows when their sums meet in LDS.
+template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool GATED> struct I8Block {
+    static constexpr bool SLOTS = STAGES == 0;
+    static constexpr int TM = GM * WM, TN = GN * WN, NW = GM * GN, WAVES = NW * GK, BM = WM / 16, BN = WN / 16;
+    static constexpr int A_BYTES = TM * 128, B_BYTES = TN * 128, STAGE = A_BYTES + B_BYTES;
+    static constexpr int LA = A_BYTES / NW / 1024, LB = B_BYTES / NW / 1024;
+    static constexpr int NR = BM + BN, NM = BM * BN;
+    static constexpr int RING = SLOTS ? 5 * A_BYTES : STAGES * STAGE, LDS = GK * RING;
+    static constexpr int FAR = SLOTS ? 3 : STAGES;           // the furthest copy is of tile t + FAR
+    static constexpr int AHEAD = SLOTS ? LA : (STAGES - 2) * (LA + LB);       // copies in flight beyond the next tile, steady state
+    static_assert(!SLOTS || A_BYTES == B_BYTES, "five equal slots");
+    static_assert(LDS <= 163840 && A_BYTES % (NW * 1024) == 0 && B_BYTES % (NW * 1024) == 0, "a CU's LDS; whole copies");
+    static_assert(!GATED || BN % 2 == 0, "gates and values in pairs");
+    static constexpr int KEEP = BM / GK;                     // blocks of rows that a wave stores
+    static_assert(GK == 1 || (GK == 2 && BM % 2 == 0 && NW * BM * BN * 1024 <= LDS), "two groups share out the rows");
+
+    struct Frag { i8_u32x4 a[BM], b[BN]; };
+    // r-th LDS read of k-step KS's fragments: B first (its blocks are all used by the first row of blocks)
+    template <int KS, int R> __device__ static __forceinline__ void read_one(uint32_t aa, uint32_t ba, Frag &f) {
+        if constexpr (R < BN) f.b[R] = i8_read<R * 2048>(KS ? ba ^ 64u : ba);
+        else f.a[R - BN] = i8_read<(R - BN) * 2048>(KS ? aa ^ 64u : aa);
+    }
+    template <int KS, int R, int E> __device__ static __forceinline__ void read_range(uint32_t aa, uint32_t ba, Frag &f) {
+        if constexpr (R < E && R < NR) {
+            read_one<KS, R>(aa, ba, f);
+            read_range<KS, R + 1, E>(aa, ba, f);
+        }
+    }
+    // every read of the set has arrived; its registers are produced here
+    __device__ static __forceinline__ void arrived(Frag &f) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < BM; ++i) asm volatile("" : "+v"(f.a[i]));
+#pragma unroll
+        for (int i = 0; i < BN; ++i) asm volatile("" : "+v"(f.b[i]));
+    }
+    // m-th MFMA of a k-step: rows of blocks in turn, columns back and forth, so that one operand stays
+    __device__ static __forceinline__ void mfma_one(const Frag &f, i8_i32x4 (&acc)[BM][BN], int m) {
+        const int bi = m / BN, bj = (bi & 1) ? BN - 1 - m % BN : m % BN;
+        acc[bi][bj] = i8_mfma(f.b[bj], f.a[bi], acc[bi][bj]);
+    }
+    // The MFMAs of `use`, with the reads of `fill` (k-step KS of some tile) in the first three quarters and, where COPY,
+    // LA + LB copies spread over all of them.  Pinned: left alone, the compiler gathers the reads in front.
+    template <int KS, bool COPY, int M = 0, typename F>
+    __device__ static __forceinline__ void phase(uint32_t aa, uint32_t ba, Frag &fill, const Frag &use, i8_i32x4 (&acc)[BM][BN], F copy) {
+        read_range<KS, M * NR * 4 / (NM * 3), (M + 1) * NR * 4 / (NM * 3)>(aa, ba, fill);
+        if constexpr (COPY) i8_each<M *(LA + LB) / NM, (M + 1) * (LA + LB) / NM>(copy);
+        mfma_one(use, acc, M);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (M + 1 < NM) phase<KS, COPY, M + 1>(aa, ba, fill, use, acc, copy);
+    }
+
+    // Where a tile's operands lie.  Copies: wave instruction i fills 1 KB, eight rows, of the tile.  A row that is not there, and what lies beyond the
+    // last one, reads as zeros by the buffer's bound; bytes beyond K are whatever follows, and are cut from A's fragments.
+    struct Source {
+        __amdgpu_buffer_rsrc_t a;
+        I8Columns<TN, GATED> cols;
+        uint32_t off_a[LA], off_b[LB];
+        // (wave: in its group; t: a group's k-tile, which is the block's k-tile GK * t + group)
+        __device__ __forceinline__ Source(const I8Args &g, const I8Tile &tile, uint32_t wave, uint32_t lane) : cols(g, tile) {
+            a = GROUPED ? i8_rsrc(g.A, g.a_rows * g.lda) : i8_rsrc(g.A + (uint64_t)tile.row0 * g.lda, tile.rows * g.lda);
+#pragma unroll
+            for (int i = 0; i < LA; ++i) {
+                const uint32_t row = wave * (LA * 8) + i * 8 + lane / 8u, kc = (lane & 7u) ^ i8_swizzle(row);
+                if constexpr (GROUPED) {
+                    const uint32_t s = row < tile.rows ? i8_source<true>(g, tile.row0 + row) : ~0u;
+                    off_a[i] = s == ~0u ? kOutside : s * g.lda + kc * 16u;
+                } else off_a[i] = row * g.lda + kc * 16u;
+            }
+#pragma unroll
+            for (int i = 0; i < LB; ++i) {
+                const uint32_t row = wave * (LB * 8) + i * 8 + lane / 8u, kc = (lane & 7u) ^ i8_swizzle(row);
+                off_b[i] = ((GATED ? row / 32u * 16u + (row & 15u) : row) * g.ldb) + kc * 16u;
+            }
+        }
+        template <int I> __device__ __forceinline__ void copy_a(unsigned char *smem, uint32_t wave, uint32_t group, uint32_t t, uint32_t slot) const {
+            i8_copy(a, smem + slot + wave * (LA * 1024) + I * 1024, off_a[I], t * (128u * GK) + group * 128u);
+        }
+        template <int I> __device__ __forceinline__ void copy_b(unsigned char *smem, uint32_t wave, uint32_t group, uint32_t t, uint32_t slot) const {
+            const bool values = GATED && (((wave * (LB * 8) + I * 8) / 16u) & 1u);
+            i8_copy(values ? cols.values : cols.b, smem + slot + wave * (LB * 1024) + I * 1024, off_b[I], t * (128u * GK) + group * 128u);
+        }
+    };
+    static __device__ __forceinline__ uint32_t next_slot(uint32_t s) {
+        constexpr uint32_t STEP = SLOTS ? 2 * A_BYTES : STAGE;
+        return s + STEP >= (uint32_t)RING ? s + STEP - RING : s + STEP;
+    }
+    // the ring full
+    static __device__ __forceinline__ void fill(const Source &src, unsigned char *ring, uint32_t wave, uint32_t group, uint32_t nk) {
+        uint32_t pa = 0, pb = A_BYTES;
+#pragma unroll
+        for (int t = 0; t < FAR; ++t) {
+            if ((uint32_t)t < nk) {
+                i8_each<0, LA>([&](auto i) { src.template copy_a<decltype(i)::value>(ring, wave, group, t, pa); });
+                if (!SLOTS || t < 2) i8_each<0, LB>([&](auto i) { src.template copy_b<decltype(i)::value>(ring, wave, group, t, pb); });
+            }
+            pa = next_slot(pa); pb = next_slot(pb);
+        }
+    }
+
+    // All tiles of a workgroup.  The ring is filled for the next one while the last one's sums are scaled and stored.
+    __device__ static __forceinline__ void run(const I8Args &g, unsigned char *smem) {
+        const uint32_t tid = threadIdx.x, lane = tid & 63u, all = __builtin_amdgcn_readfirstlane(tid >> 6), wave = GK > 1 ? all % NW : all, group = GK > 1 ? all / NW : 0u;
+        unsigned char *const ring = smem + group * RING;
+        const I8Tiles<TM, TN, GROUPED> tiles(g);
+        const uint32_t nk = ((g.k + 127u) / 128u + GK - 1u) / GK;    // k-tiles of a group (the last of the second may be nothing: it is cut)
+        I8Tile tile = tiles.take(g, 0);
+        if (!tile.some) return;
+        Source src(g, tile, wave, lane);
+        fill(src, ring, wave, group, nk);
+        for (uint32_t turn = 1;; ++turn) {
+            i8_i32x4 acc[BM][BN];
+#pragma unroll
+            for (int i = 0; i < BM; ++i)
+#pragma unroll
+                for (int j = 0; j < BN; ++j) acc[i][j] = i8_i32x4{0, 0, 0, 0};
+            const I8Tile next = products(g, src, ring, wave, group, lane, nk, acc, [&] { return tiles.take(g, turn); });
+            const I8Tile done = tile;
+            const I8Columns<TN, GATED> cols = src.cols;
+            if constexpr (GK == 1) {
+                if (next.some) {
+                    // (every wave has read the last k-tile: they met after its second k-step had arrived)
+                    src = Source(g, next, wave, lane);
+                    fill(src, ring, wave, group, nk);
+                }
+                results(g, done, cols, (wave / GN) * WM, wave % GN, lane, acc);
+            } else {
+                i8_i32x4 kept[KEEP][BN];
+                meet(smem, wave, group, lane, acc, kept);
+                if (next.some) {
+                    __syncthreads();                                 // the sums have been read
+                    src = Source(g, next, wave, lane);
+                    fill(src, ring, wave, group, nk);
+                }
+                results(g, done, cols, (wave / GN) * WM + group * (KEEP * 16), wave % GN, lane, kept);
+            }
+            if (!next.some) return;
+            tile = next;
+        }
+    }
+
+    // The two groups' sums: each wave gives the rows away that the other one's wave of the same place keeps.
+    __device__ static __forceinline__ void meet(unsigned char *smem, uint32_t wave, uint32_t group, uint32_t lane, const i8_i32x4 (&acc)[BM][BN], i8_i32x4 (&kept)[KEEP][BN]) {
+        i8_i32x4 *const sums = reinterpret_cast<i8_i32x4 *>(smem);
+        const uint32_t give = ((1u - group) * NW + wave) * (KEEP * BN * 64u) + lane, take = (group * NW + wave) * (KEEP * BN * 64u) + lane;
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i)
+#pragma unroll
+            for (int j = 0; j < BN; ++j) {
+                const i8_i32x4 low = acc[i][j], high = acc[BM - KEEP + i][j];
+                sums[give + (i * BN + j) * 64u] = group ? low : high;
+                kept[i][j] = group ? high : low;
+            }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i)
+#pragma unroll
+            for (int j = 0; j < BN; ++j) kept[i][j] += sums[take + (i * BN + j) * 64u];
+    }
+
+    template <typename NEXT>
+    __device__ static __forceinline__ I8Tile products(const I8Args &g, const Source &src, unsigned char *ring, uint32_t wave, uint32_t group, uint32_t lane, uint32_t nk, i8_i32x4 (&acc)[BM][BN], NEXT next) {
+        const uint32_t wm = wave / GN, wn = wave % GN;
+        const uint32_t sbase = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)ring;
+        const uint32_t ra = wm * WM + (lane & 15u), rb = wn * WN + (lane & 15u);
+        const uint32_t fa = sbase + ra * 128u + (((lane >> 4) ^ i8_swizzle(ra)) << 4);
+        const uint32_t fb = sbase + rb * 128u + (((lane >> 4) ^ i8_swizzle(rb)) << 4);
+        uint32_t sa = 0, sb = A_BYTES;                               // slots of the tile being consumed
+        constexpr int BEHIND = SLOTS ? 2 * LA + LB : (STAGES - 1) * (LA + LB);         // copies behind k-tile 0; the last results' stores may be behind it too
+        if (nk >= (uint32_t)FAR) i8_wait_copies<BEHIND>();
+        else i8_wait_copies<0>();
+        __builtin_amdgcn_s_barrier();
+        Frag f0, f1;
+        read_range<0, 0, NR>(fa + sa, fb + sb, f0);
+        auto step = [&](uint32_t t, auto steady_c) {
+            constexpr bool STEADY = decltype(steady_c)::value;        // every copy of the steady state is due
+            arrived(f0);
+            if constexpr (!STEADY) {
+                const uint32_t k0 = (t * GK + group) * 128u;
+                if (k0 + 128u > g.k) {
+#pragma unroll
+                    for (int i = 0; i < BM; ++i) f0.a[i] = i8_cut(f0.a[i], k0 + (lane >> 4) * 16u, g.k);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            phase<1, false>(fa + sa, fb + sb, f1, f0, acc, [](auto) {});
+            arrived(f1);
+            if constexpr (!STEADY) {
+                const uint32_t k0 = (t * GK + group) * 128u;
+                if (k0 + 128u > g.k) {
+#pragma unroll
+                    for (int i = 0; i < BM; ++i) f1.a[i] = i8_cut(f1.a[i], k0 + 64u + (lane >> 4) * 16u, g.k);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            // Tile t's LDS has been read by this wave; tile t + 1 must have landed.  In flight beyond it: A of t + 2 (slots), or
+            // the stages up to t + STAGES - 1.
+            const uint32_t behind = nk - 1u - t;                      // tiles after t
+            if (STEADY || (SLOTS ? behind >= 2u : behind >= (uint32_t)STAGES - 1u)) i8_wait_copies<AHEAD>();
+            else i8_wait_copies<0>();
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            const uint32_t na = next_slot(sa), nb = next_slot(sb);
+            // (past the last tile the reads fetch what happens to be there, for nobody)
+            if constexpr (SLOTS) {
+                const bool more_b = STEADY || t + 2u < nk;
+                phase<0, true>(fa + na, fb + nb, f0, f1, acc, [&](auto q) {
+                    constexpr int Q = decltype(q)::value;
+                    if constexpr (Q < LB) { if (more_b) src.template copy_b<Q>(ring, wave, group, t + 2u, sa); }
+                    else if constexpr (STEADY) src.template copy_a<Q - LB>(ring, wave, group, t + 3u, sb);
+                });
+            } else {
+                phase<0, STEADY>(fa + na, fb + nb, f0, f1, acc, [&](auto q) {
+                    constexpr int Q = decltype(q)::value;
+                    if constexpr (Q < LA) src.template copy_a<Q>(ring, wave, group, t + STAGES, sa);
+                    else src.template copy_b<Q - LA>(ring, wave, group, t + STAGES, sb);
+                });
+            }
+            sa = na; sb = nb;
+        };
+        uint32_t t = 0;
+        for (; t + FAR < nk; ++t) step(t, std::true_type{});
+        const I8Tile after = next();
+        for (; t < nk; ++t) step(t, std::false_type{});
+        arrived(f0);                                                  // nothing of the last reads outlives the loop
+        return after;
+    }
+
+    // Sums to C: lane l holds row l % 16, columns 4 * (l / 16) .. + 3 of every 16 x 16 block, the first at row `row`, wave column wn
+    template <int NI>
+    __device__ static __forceinline__ void results(const I8Args &g, const I8Tile &tile, const I8Columns<TN, GATED> &cols, uint32_t row, uint32_t wn, uint32_t lane, const i8_i32x4 (&acc)[NI][BN]) {
+        const uint32_t r0 = row + (lane & 15u), q4 = lane >> 4;
+        float sr[NI];
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const uint32_t r = r0 + i * 16u, s = r < tile.rows ? i8_source<GROUPED>(g, tile.row0 + r) : ~0u;
+            sr[i] = s == ~0u ? 0.f : g.scale_a[s];
+        }
+        constexpr int PER = GATED ? 2 : 1, NP = BN / PER;             // blocks of columns of C
+        const uint32_t c0 = cols.first + wn * (WN / PER) + q4 * 4u;
+        I8Scales<GATED> scales[NP];
+#pragma unroll
+        for (int j = 0; j < NP; ++j) {
+            const uint32_t col = c0 + j * 16u;
+            scales[j].load(cols, g, tile, col < cols.of_c ? col : cols.of_c - 1u);
+        }
+        auto value = [&](int i, int j) -> i8_f32x4 {
+            if constexpr (GATED) return i8_gated(scales[j], sr[i], acc[i][2 * j], acc[i][2 * j + 1]);
+            else return i8_scaled(scales[j], sr[i], acc[i][j]);
+        };
+        bool pairs = false;
+        if constexpr (NP % 2 == 0) pairs = g.vec && g.out_kind != 0;
+        if (pairs) {
+            // two neighbouring blocks: after the swap of odd and even 16-lane rows a lane holds 8 columns of one of them
+            uint16_t *const C = static_cast<uint16_t *>(g.C);
+            const uint32_t cc = cols.first + wn * (WN / PER) + (q4 & 1u) * 16u + (q4 >> 1) * 8u;
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+#pragma unroll
+                for (int j = 0; j + 1 < NP; j += 2) {
+                    const i8_f32x4 x = value(i, j), y = value(i, j + 1);
+                    const auto lo = __builtin_amdgcn_permlane16_swap(i8_pack(g.out_kind, x[0], x[1]), i8_pack(g.out_kind, y[0], y[1]), false, false);
+                    const auto hi = __builtin_amdgcn_permlane16_swap(i8_pack(g.out_kind, x[2], x[3]), i8_pack(g.out_kind, y[2], y[3]), false, false);
+                    const i8_u32x4 v = {lo[0], hi[0], lo[1], hi[1]};
+                    const uint32_t r = r0 + i * 16u, c = cc + j * 16u;
+                    if (r < tile.rows && c < cols.of_c) *reinterpret_cast<i8_u32x4 *>(C + (uint64_t)(tile.row0 + r) * g.ldc + c) = v;
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+#pragma unroll
+                for (int j = 0; j < NP; ++j) {
+                    const uint32_t r = r0 + i * 16u, col = c0 + j * 16u;
+                    if (r < tile.rows && col < cols.of_c) i8_store4(g, tile.row0 + r, col, cols.of_c, value(i, j));
+                }
+        }
+    }
+};
+
+template <typename BODY, int WAVES_PER_SIMD> __global__ __launch_bounds__(BODY::WAVES * 64, WAVES_PER_SIMD) void ft_i8_block(I8Args a) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    BODY::run(a, smem);
+}
+
+}  // namespace ftk
+
+using namespace ftk;
+
+namespace {
+
+// PER_CU workgroups fit a CU: as many are launched as the device holds, and take the tiles in turn
+template <typename BODY, int PER_CU, bool GROUPED> ft_status launch(I8Args &a, hipStream_t s) {
+    constexpr auto KERNEL = &ft_i8_block<BODY, BODY::WAVES / 4 * PER_CU>;
+    const hipError_t e = raise_lds_limit<KERNEL>();
+    if (e != hipSuccess) { ftd_set_hip_error((int)e); return FT_ERR_HIP; }
+    if (!i8_grid(a, BODY::TM, BODY::TN, GROUPED)) return FT_ERR_UNSUPPORTED;
+    const uint32_t tiles = a.row_tiles * a.col_tiles, most = a.cus * PER_CU;
+    hipLaunchKernelGGL(KERNEL, dim3(tiles < most ? tiles : most), dim3(BODY::WAVES * 64), BODY::LDS, s, a);
+    return op_launched();
+}
+template <bool GROUPED, bool GATED> ft_status run(I8Kind kind, I8Args &a, hipStream_t s) {
+    switch (kind) {
+        case I8_256x256: return launch<I8Block<128, 64, 2, 4, 1, 0, GROUPED, GATED>, 1, GROUPED>(a, s);
+        case I8_128x256: return launch<I8Block<64, 64, 2, 4, 1, 3, GROUPED, GATED>, 1, GROUPED>(a, s);
+        case I8_128x128: return launch<I8Block<64, 64, 2, 2, 1, 2, GROUPED, GATED>, 2, GROUPED>(a, s);
+        case I8_64x128: return launch<I8Block<32, 64, 2, 2, 1, 3, GROUPED, GATED>, 2, GROUPED>(a, s);
+        default: return launch<I8Block<32, 32, 2, 2, 2, 4, GROUPED, GATED>, 1, GROUPED>(a, s);
+    }
+}
+
+}  // namespace
+
+namespace ftk {
+
+ft_status i8_launch_blocks(I8Kind kind, bool grouped, I8Args &a, void *stream) {
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (grouped) return a.gated ? run<true, true>(kind, a, s) : run<true, false>(kind, a, s);
+    return a.gated ? run<false, true>(kind, a, s) : run<false, false>(kind, a, s);
+}
+
+}  // namespace ftk

@@ -12,205 +12,23 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include <type_traits>
+#include <atomic>
 
 #include "ft_internal.h"
-#include "i8_ops.h"
-#include "lane_types.h"
-#include "lds_limit.h"
+#include "i8_blocks.h"
+#include "i8_tile.h"
 #include "op_launch.h"
 
 namespace ftk {
-
-typedef int32_t i8_i32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t i8_u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t i8_u32x2 __attribute__((ext_vector_type(2)));
-typedef float i8_f32x2 __attribute__((ext_vector_type(2)));
-typedef float i8_f32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 i8_bf16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 i8_f16x2 __attribute__((ext_vector_type(2)));
-
-constexpr uint32_t kOutside = 0x80000000u;          // an offset beyond every buffer: reads as zeros
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t i8_rsrc(const int8_t *p, uint32_t bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(p), 0, (int)bytes, 0x00020000);
-}
-__device__ __forceinline__ i8_u32x4 i8_load(__amdgpu_buffer_rsrc_t r, uint32_t off) {
-    return __builtin_bit_cast(i8_u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0));
-}
-__device__ __forceinline__ i8_i32x4 i8_mfma(i8_u32x4 b, i8_u32x4 a, i8_i32x4 c) {
-    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i8_i32x4, b), __builtin_bit_cast(i8_i32x4, a), c, 0, 0, 0);
-}
-// the bytes of a fragment at k .. k + 15 that lie before K
-__device__ __forceinline__ i8_u32x4 i8_cut(i8_u32x4 v, uint32_t k, uint32_t K) {
-    const int left = (int)K - (int)k;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int n = left - 4 * i;                          // bytes of this word
-        v[i] = n >= 4 ? v[i] : n <= 0 ? 0u : v[i] & ((1u << (8 * n)) - 1u);
-    }
-    return v;
-}
-
-// Where a workgroup's tile lies: rows row0 .. row0 + rows - 1 of C, columns n0 .., weight `expert`.
-struct I8Tile {
-    uint32_t row0, rows, n0, expert;
-    bool some;                                               // false: nothing left for this workgroup
-};
-
-// Every XCD (workgroup b runs on XCD b % 8) takes one contiguous run of the `total` tiles: those that share a panel of B meet in one L2.
-__device__ __forceinline__ bool i8_position(uint32_t b, uint32_t total, uint32_t *u) {
-    const uint32_t x = b & 7u, j = b >> 3, q = total >> 3, r = total & 7u;
-    *u = x * q + (x < r ? x : r) + j;
-    return j < q + (x < r ? 1u : 0u);
-}
-
-template <int TM, int TN, bool GROUPED> __device__ __forceinline__ I8Tile i8_tile(const I8Args &a, uint32_t b) {
-    I8Tile t;
-    uint32_t u;
-    if constexpr (!GROUPED) {
-        t.some = i8_position(b, a.row_tiles * a.col_tiles, &u);
-        // bands of `group` rows of tiles, column by column
-        const uint32_t band = u / (a.group * a.col_tiles), w = u - band * a.group * a.col_tiles;
-        const uint32_t high = a.row_tiles - band * a.group < a.group ? a.row_tiles - band * a.group : a.group;
-        const uint32_t col = w / high;
-        t.row0 = (band * a.group + w - col * high) * TM;
-        t.rows = a.m - t.row0 < (uint32_t)TM ? a.m - t.row0 : (uint32_t)TM;
-        t.n0 = col * TN;
-        t.expert = 0;
-        return t;
-    } else {
-        // Each lane counts the row tiles of an expert; prefix sums over the lanes say whose tile this is.
-        const uint32_t lane = threadIdx.x & 63u;
-        auto group = [&](uint32_t e, uint32_t *beg) -> uint32_t {       // rows of expert e
-            if (e >= a.experts) { *beg = 0; return 0u; }
-            int32_t s = a.offsets[e], n = a.offsets[e + 1];
-            s = s < 0 ? 0 : s > (int32_t)a.m ? (int32_t)a.m : s;
-            n = n < s ? s : n > (int32_t)a.m ? (int32_t)a.m : n;
-            *beg = (uint32_t)s;
-            return (uint32_t)(n - s);
-        };
-        auto scan = [&](uint32_t v) -> uint32_t {
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const uint32_t up = __shfl_up(v, d);
-                if (lane >= (uint32_t)d) v += up;
-            }
-            return v;
-        };
-        uint32_t beg, count = group(lane, &beg), tiles = (count + TM - 1u) / TM, upto = scan(tiles);
-        uint32_t total = __builtin_amdgcn_readlane(upto, 63);
-        for (uint32_t at = 64; at < a.experts; at += 64u) {
-            uint32_t skip;
-            total += __builtin_amdgcn_readlane(scan((group(at + lane, &skip) + TM - 1u) / TM), 63);
-        }
-        t.some = i8_position(b, total * a.col_tiles, &u);
-        t.row0 = t.rows = t.n0 = t.expert = 0;
-        if (!t.some) return t;
-        uint32_t before = 0;
-        for (uint32_t at = 0;; at += 64u) {
-            if (at) {
-                count = group(at + lane, &beg);
-                tiles = (count + TM - 1u) / TM;
-                upto = scan(tiles);
-            }
-            const uint64_t behind = __ballot((before + upto) * a.col_tiles > u);
-            if (behind) {
-                const int l = __builtin_ctzll(behind);
-                const uint32_t n_tiles = __builtin_amdgcn_readlane(tiles, l), w = u - (before + __builtin_amdgcn_readlane(upto, l) - n_tiles) * a.col_tiles;
-                const uint32_t col = w / n_tiles, row = w - col * n_tiles, rows = __builtin_amdgcn_readlane(count, l) - row * TM;
-                t.expert = at + (uint32_t)l;
-                t.row0 = __builtin_amdgcn_readlane(beg, l) + row * TM;
-                t.rows = rows < (uint32_t)TM ? rows : (uint32_t)TM;
-                t.n0 = col * TN;
-                t.some = col < a.col_tiles;                  // (offsets that are not ascending can say otherwise)
-                return t;
-            }
-            before += __builtin_amdgcn_readlane(upto, 63);
-            if (at + 64u >= a.experts) { t.some = false; return t; }    // (not reached: u < total * col_tiles)
-        }
-    }
-}
-
-// Row of A that row r of C takes; one that is not there: ~0
-template <bool GROUPED> __device__ __forceinline__ uint32_t i8_source(const I8Args &a, uint32_t r) {
-    if constexpr (!GROUPED) return r;
-    const uint32_t s = a.a_row ? (uint32_t)a.a_row[r] : r;
-    return s < a.a_rows ? s : ~0u;
-}
-
-// A tile's columns: where their rows of B begin, for blocks of 16, and their places in C
-template <int TN, bool GATED> struct I8Columns {
-    __amdgpu_buffer_rsrc_t b, values;
-    uint32_t first, of_c;                                    // first column of the tile in C, columns of C
-    __device__ __forceinline__ I8Columns(const I8Args &a, const I8Tile &t) {
-        const int8_t *const w = a.B + (uint64_t)t.expert * a.n * a.ldb;
-        constexpr uint32_t WIDTH = GATED ? TN / 2 : TN;
-        first = GATED ? t.n0 / 2u : t.n0;
-        of_c = GATED ? a.n / 2u : a.n;
-        const uint32_t rows = of_c - first < WIDTH ? of_c - first : WIDTH;
-        b = i8_rsrc(w + (uint64_t)first * a.ldb, rows * a.ldb);
-        values = GATED ? i8_rsrc(w + (uint64_t)(of_c + first) * a.ldb, rows * a.ldb) : b;
-    }
-    __device__ __forceinline__ uint32_t row_of_block(int j) const { return (GATED ? j / 2 : j) * 16u; }
-    __device__ __forceinline__ __amdgpu_buffer_rsrc_t operand(int j) const { return GATED && j % 2 ? values : b; }
-};
-template <typename COLS> __device__ __forceinline__ i8_f32x4 i8_scaled(const COLS &cols, const I8Args &a, const I8Tile &t, uint32_t col, float sa, i8_i32x4 v) {
-    const uint64_t at = (uint64_t)t.expert * a.n;
-    i8_f32x4 out;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const uint64_t c = at + (col + e < cols.of_c ? col + e : col);
-        out[e] = (float)v[e] * sa * a.scale_b[c];
-        if (a.bias) out[e] += a.bias[c];
-    }
-    return out;
-}
-template <typename COLS> __device__ __forceinline__ i8_f32x4 i8_gated(const COLS &cols, const I8Args &a, const I8Tile &t, uint32_t col, float sa, i8_i32x4 g, i8_i32x4 u) {
-    const uint64_t at = (uint64_t)t.expert * a.n;
-    i8_f32x4 out;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const uint64_t c = at + (col + e < cols.of_c ? col + e : col);
-        out[e] = silu_mul((float)g[e] * sa * a.scale_b[c], (float)u[e] * sa * a.scale_b[c + cols.of_c]);
-    }
-    return out;
-}
-
-// Four neighbouring columns of a row of C
-__device__ __forceinline__ void i8_store4(const I8Args &a, uint32_t row, uint32_t col, uint32_t columns, i8_f32x4 v) {
-    const uint64_t at = (uint64_t)row * a.ldc + col;
-    if (a.out_kind == 0) {
-        float *const c = static_cast<float *>(a.C) + at;
-        if (a.vec) *reinterpret_cast<i8_f32x4 *>(c) = v;
-        else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (col + e < columns) c[e] = v[e];
-        }
-    } else {
-        uint16_t *const c = static_cast<uint16_t *>(a.C) + at;
-        i8_u32x2 h;
-        if (a.out_kind == 1) h = i8_u32x2{__builtin_bit_cast(uint32_t, i8_f16x2{(_Float16)v[0], (_Float16)v[1]}), __builtin_bit_cast(uint32_t, i8_f16x2{(_Float16)v[2], (_Float16)v[3]})};
-        else h = i8_u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(i8_f32x2{v[0], v[1]}, i8_bf16x2)),
-                          __builtin_bit_cast(uint32_t, __builtin_convertvector(i8_f32x2{v[2], v[3]}, i8_bf16x2))};
-        if (a.vec) *reinterpret_cast<i8_u32x2 *>(c) = h;
-        else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (col + e < columns) c[e] = (uint16_t)(h[e / 2] >> (e % 2 * 16));
-        }
-    }
-}
 
 // Few rows: tiles of 16 MB x 16 NB whose W waves take turns along the reduce axis, 128 bytes of it at a time, straight from memory into the
 // matrix cores' operands; their sums meet in LDS.  Every byte of either operand is loaded by one wave of a workgroup once.
 template <int MB, int NB, int W, int AHEAD, bool GROUPED, bool GATED> __global__ __launch_bounds__(W * 64) void ft_i8_stream(I8Args a) {
     static_assert(!GATED || NB % 2 == 0, "gates and values in pairs");
-    extern __shared__ i8_i32x4 sums[];                       // [W][MB * NB][64]
+    __shared__ i8_i32x4 sums[W * MB * NB * 64];
     constexpr int TM = MB * 16, TN = NB * 16;
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u);
-    const I8Tile t = i8_tile<TM, TN, GROUPED>(a, blockIdx.x);
+    const I8Tile t = I8Tiles<TM, TN, GROUPED>(a).take(a, 0);
     if (!t.some) return;
     const __amdgpu_buffer_rsrc_t ar = GROUPED ? i8_rsrc(a.A, a.a_rows * a.lda) : i8_rsrc(a.A + (uint64_t)t.row0 * a.lda, t.rows * a.lda);
     const I8Columns<TN, GATED> cols(a, t);
@@ -286,10 +104,10 @@ template <int MB, int NB, int W, int AHEAD, bool GROUPED, bool GATED> __global__
         };
         const uint32_t s = i8_source<GROUPED>(a, t.row0 + r);
         const float sa = s == ~0u ? 0.f : a.scale_a[s];
-        i8_f32x4 out;
-        if constexpr (GATED) out = i8_gated(cols, a, t, col, sa, sum(2u * j), sum(2u * j + 1u));
-        else out = i8_scaled(cols, a, t, col, sa, sum(j));
-        i8_store4(a, t.row0 + r, col, cols.of_c, out);
+        I8Scales<GATED> scales;
+        scales.load(cols, a, t, col);
+        if constexpr (GATED) i8_store4(a, t.row0 + r, col, cols.of_c, i8_gated(scales, sa, sum(2u * j), sum(2u * j + 1u)));
+        else i8_store4(a, t.row0 + r, col, cols.of_c, i8_scaled(scales, sa, sum(j)));
     }
 }
 
@@ -300,27 +118,30 @@ using namespace ftk;
 namespace {
 
 template <int MB, int NB, int W, int AHEAD, bool GROUPED, bool GATED> ft_status launch_stream(I8Args &a, hipStream_t s) {
-    constexpr uint32_t TM = MB * 16, TN = NB * 16;
-    // (grouped: every group but the last row tile of each is full)
-    const uint64_t rows = GROUPED ? (uint64_t)a.m / TM + (a.experts < a.m ? a.experts : a.m) : ((uint64_t)a.m + TM - 1) / TM;
-    a.col_tiles = (a.n + TN - 1) / TN;
-    if (rows * a.col_tiles > 0x7fffffffull) return FT_ERR_UNSUPPORTED;
-    a.row_tiles = (uint32_t)rows;
-    a.group = a.row_tiles < 16u ? a.row_tiles : 16u;
-    hipLaunchKernelGGL((ft_i8_stream<MB, NB, W, AHEAD, GROUPED, GATED>), dim3(a.row_tiles * a.col_tiles), dim3(W * 64), W * MB * NB * 1024u, s, a);
+    if (!i8_grid(a, MB * 16, NB * 16, GROUPED)) return FT_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((ft_i8_stream<MB, NB, W, AHEAD, GROUPED, GATED>), dim3(a.row_tiles * a.col_tiles), dim3(W * 64), 0, s, a);
     return op_launched();
 }
-template <bool GROUPED, bool GATED> ft_status run(I8Args &a, hipStream_t s) {
-    const uint32_t rows = GROUPED ? (a.m + a.experts - 1u) / a.experts : a.m;         // of a group, if they are alike
-    if (rows <= 16u) return launch_stream<1, GATED ? 2 : 1, 8, 2, GROUPED, GATED>(a, s);
-    if (rows <= 32u) return launch_stream<2, 2, 8, 2, GROUPED, GATED>(a, s);
-    return launch_stream<4, 2, 8, 1, GROUPED, GATED>(a, s);
+// compute units of the current device
+int compute_units() {
+    static std::atomic<int> known[64];
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
+    n = known[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
+        known[dev].store(n, std::memory_order_relaxed);
+    }
+    return n;
 }
 template <bool GROUPED> ft_status run(I8Args &a, void *stream) {
     const ft_status st = op_stream_check(stream);
     if (st != FT_OK) return st;
+    a.cus = (uint32_t)compute_units();
+    const I8Kind kind = i8_choose(a, GROUPED);
+    if (kind != I8_STREAM) return i8_launch_blocks(kind, GROUPED, a, stream);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return a.gated ? run<GROUPED, true>(a, s) : run<GROUPED, false>(a, s);
+    return a.gated ? launch_stream<1, 2, 8, 2, GROUPED, true>(a, s) : launch_stream<1, 1, 8, 2, GROUPED, false>(a, s);
 }
 
 }  // namespace

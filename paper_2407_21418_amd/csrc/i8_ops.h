@@ -52,6 +52,7 @@ struct I8Args {
     uint32_t vec;                        // rows of C can be written 16 bytes (8 where C has 16 bits) at a time
     uint32_t row_tiles, col_tiles;       // grid of the body that was chosen (grouped: the most row tiles there can be)
     uint32_t group;
+    uint32_t cus;                        // compute units of the device
 };
 inline ft_status i8_check(const ft_i8_desc *d, bool grouped, uint32_t m, const int32_t *offsets, const int8_t *A, const float *scale_a, uint32_t a_rows,
                           const int32_t *a_row, const int8_t *B, const float *scale_b, const float *bias, void *C, I8Args *a, bool *launch) {

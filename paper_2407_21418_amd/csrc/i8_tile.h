@@ -1,0 +1,210 @@
+// Matmuls in 8-bit integers: what the kernels of i8_gemm.hip and i8_blocks.hip share -- which tile a workgroup takes, where its operands
+// lie, and what becomes of its sums.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "i8_ops.h"
+#include "lane_types.h"
+
+namespace ftk {
+
+typedef int32_t i8_i32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t i8_u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t i8_u32x2 __attribute__((ext_vector_type(2)));
+typedef float i8_f32x2 __attribute__((ext_vector_type(2)));
+typedef float i8_f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 i8_bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 i8_f16x2 __attribute__((ext_vector_type(2)));
+
+constexpr uint32_t kOutside = 0x80000000u;          // an offset beyond every buffer: reads as zeros
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t i8_rsrc(const int8_t *p, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(p), 0, (int)bytes, 0x00020000);
+}
+__device__ __forceinline__ i8_u32x4 i8_load(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+    return __builtin_bit_cast(i8_u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0));
+}
+__device__ __forceinline__ i8_i32x4 i8_mfma(i8_u32x4 b, i8_u32x4 a, i8_i32x4 c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i8_i32x4, b), __builtin_bit_cast(i8_i32x4, a), c, 0, 0, 0);
+}
+// the bytes of a fragment at k .. k + 15 that lie before K
+__device__ __forceinline__ i8_u32x4 i8_cut(i8_u32x4 v, uint32_t k, uint32_t K) {
+    const int left = (int)K - (int)k;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int n = left - 4 * i;                          // bytes of this word
+        v[i] = n >= 4 ? v[i] : n <= 0 ? 0u : v[i] & ((1u << (8 * n)) - 1u);
+    }
+    return v;
+}
+
+// Where a workgroup's tile lies: rows row0 .. row0 + rows - 1 of C, columns n0 .., weight `expert`.
+struct I8Tile {
+    uint32_t row0, rows, n0, expert;
+    bool some;                                               // false: nothing left for this workgroup
+};
+
+// Every XCD (workgroup b of the grid runs on XCD b % 8) takes one contiguous run of the `total` tiles, so that those which share a panel of B
+// meet in one L2; its workgroups take the run's tiles in turn.  u: the place of workgroup b's `turn`-th tile.
+__device__ __forceinline__ bool i8_position(uint32_t b, uint32_t grid, uint32_t turn, uint32_t total, uint32_t *u) {
+    const uint32_t x = b & 7u, q = total >> 3, r = total & 7u, mine = (grid - x + 7u) >> 3, j = (b >> 3) + turn * mine;
+    *u = x * q + (x < r ? x : r) + j;
+    return j < q + (x < r ? 1u : 0u);
+}
+
+// The tiles of a launch.  By expert the counts of each are on the device: the lanes of a wave hold the experts' rows and prefix sums of
+// their row tiles (64 experts at a time).
+template <int TM, int TN, bool GROUPED> struct I8Tiles {
+    uint32_t total;
+    __device__ __forceinline__ I8Tiles(const I8Args &a) {
+        if constexpr (!GROUPED) total = a.row_tiles * a.col_tiles;
+        else {
+            uint32_t sum = 0, beg;
+            for (uint32_t at = 0; at < a.experts; at += 64u) sum += __builtin_amdgcn_readlane(scan((rows_of(a, at + (threadIdx.x & 63u), &beg) + TM - 1u) / TM), 63);
+            total = sum * a.col_tiles;
+        }
+    }
+    // rows of expert e, from offsets that are held to 0 .. m
+    static __device__ __forceinline__ uint32_t rows_of(const I8Args &a, uint32_t e, uint32_t *beg) {
+        if (e >= a.experts) { *beg = 0; return 0u; }
+        int32_t s = a.offsets[e], n = a.offsets[e + 1];
+        s = s < 0 ? 0 : s > (int32_t)a.m ? (int32_t)a.m : s;
+        n = n < s ? s : n > (int32_t)a.m ? (int32_t)a.m : n;
+        *beg = (uint32_t)s;
+        return (uint32_t)(n - s);
+    }
+    static __device__ __forceinline__ uint32_t scan(uint32_t v) {
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const uint32_t up = __shfl_up(v, d);
+            if ((threadIdx.x & 63u) >= (uint32_t)d) v += up;
+        }
+        return v;
+    }
+    __device__ __forceinline__ I8Tile take(const I8Args &a, uint32_t turn) const {
+        I8Tile t;
+        uint32_t u;
+        t.some = i8_position(blockIdx.x, gridDim.x, turn, total, &u);
+        t.row0 = t.rows = t.n0 = t.expert = 0;
+        if (!t.some) return t;
+        if constexpr (!GROUPED) {
+            // bands of `group` rows of tiles, column by column
+            const uint32_t band = u / (a.group * a.col_tiles), w = u - band * a.group * a.col_tiles;
+            const uint32_t high = a.row_tiles - band * a.group < a.group ? a.row_tiles - band * a.group : a.group;
+            const uint32_t col = w / high;
+            t.row0 = (band * a.group + w - col * high) * TM;
+            t.rows = a.m - t.row0 < (uint32_t)TM ? a.m - t.row0 : (uint32_t)TM;
+            t.n0 = col * TN;
+            return t;
+        }
+        uint32_t before = 0;
+        for (uint32_t at = 0; at < a.experts; at += 64u) {
+            uint32_t beg;
+            const uint32_t count = rows_of(a, at + (threadIdx.x & 63u), &beg), tiles = (count + TM - 1u) / TM, upto = scan(tiles);
+            const uint64_t behind = __ballot((before + upto) * a.col_tiles > u);
+            if (behind) {
+                const int l = __builtin_ctzll(behind);
+                const uint32_t n_tiles = __builtin_amdgcn_readlane(tiles, l), w = u - (before + __builtin_amdgcn_readlane(upto, l) - n_tiles) * a.col_tiles;
+                const uint32_t col = w / n_tiles, row = w - col * n_tiles, rows = __builtin_amdgcn_readlane(count, l) - row * TM;
+                t.expert = at + (uint32_t)l;
+                t.row0 = __builtin_amdgcn_readlane(beg, l) + row * TM;
+                t.rows = rows < (uint32_t)TM ? rows : (uint32_t)TM;
+                t.n0 = col * TN;
+                t.some = col < a.col_tiles;                  // (offsets that are not ascending can say otherwise)
+                return t;
+            }
+            before += __builtin_amdgcn_readlane(upto, 63);
+        }
+        t.some = false;                                      // (not reached: u < total)
+        return t;
+    }
+};
+
+// Row of A that row r of C takes; one that is not there: ~0
+template <bool GROUPED> __device__ __forceinline__ uint32_t i8_source(const I8Args &a, uint32_t r) {
+    if constexpr (!GROUPED) return r;
+    const uint32_t s = a.a_row ? (uint32_t)a.a_row[r] : r;
+    return s < a.a_rows ? s : ~0u;
+}
+
+// A tile's columns: where their rows of B begin, for blocks of 16, and their places in C
+template <int TN, bool GATED> struct I8Columns {
+    __amdgpu_buffer_rsrc_t b, values;
+    uint32_t first, of_c;                                    // first column of the tile in C, columns of C
+    __device__ __forceinline__ I8Columns(const I8Args &a, const I8Tile &t) {
+        const int8_t *const w = a.B + (uint64_t)t.expert * a.n * a.ldb;
+        constexpr uint32_t WIDTH = GATED ? TN / 2 : TN;
+        first = GATED ? t.n0 / 2u : t.n0;
+        of_c = GATED ? a.n / 2u : a.n;
+        const uint32_t rows = of_c - first < WIDTH ? of_c - first : WIDTH;
+        b = i8_rsrc(w + (uint64_t)first * a.ldb, rows * a.ldb);
+        values = GATED ? i8_rsrc(w + (uint64_t)(of_c + first) * a.ldb, rows * a.ldb) : b;
+    }
+    __device__ __forceinline__ uint32_t row_of_block(int j) const { return (GATED ? j / 2 : j) * 16u; }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t operand(int j) const { return GATED && j % 2 ? values : b; }
+};
+// four neighbouring values of a vector of `n`, at any alignment; beyond its end the first of them again
+struct __attribute__((packed, aligned(4))) I8Four {
+    i8_f32x4 v;
+};
+__device__ __forceinline__ i8_f32x4 i8_four(const float *p, uint32_t at, uint32_t n) {
+    if (at + 4u <= n) return reinterpret_cast<const I8Four *>(p + at)->v;
+    i8_f32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = p[at + e < n ? at + e : at];
+    return v;
+}
+// What four neighbouring columns of a tile are scaled with: read before anything is stored, which may lie anywhere for all the compiler knows
+template <bool GATED> struct I8Scales {
+    i8_f32x4 b, other;                                       // scales; the bias, or the scales of the values
+    template <typename COLS> __device__ __forceinline__ void load(const COLS &cols, const I8Args &a, const I8Tile &t, uint32_t col) {
+        const float *const sb = a.scale_b + (uint64_t)t.expert * a.n;
+        b = i8_four(sb, col, cols.of_c);
+        if constexpr (GATED) other = i8_four(sb + cols.of_c, col, cols.of_c);
+        else if (a.bias) other = i8_four(a.bias + (uint64_t)t.expert * a.n, col, cols.of_c);
+        else other = i8_f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+};
+__device__ __forceinline__ i8_f32x4 i8_scaled(const I8Scales<false> &s, float sa, i8_i32x4 v) {
+    i8_f32x4 out;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = (float)v[e] * sa * s.b[e] + s.other[e];
+    return out;
+}
+__device__ __forceinline__ i8_f32x4 i8_gated(const I8Scales<true> &s, float sa, i8_i32x4 g, i8_i32x4 u) {
+    i8_f32x4 out;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = silu_mul((float)g[e] * sa * s.b[e], (float)u[e] * sa * s.other[e]);
+    return out;
+}
+// two values rounded to 16 bits, to nearest even
+__device__ __forceinline__ uint32_t i8_pack(uint32_t out_kind, float x, float y) {
+    if (out_kind == 1) return __builtin_bit_cast(uint32_t, i8_f16x2{(_Float16)x, (_Float16)y});
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(i8_f32x2{x, y}, i8_bf16x2));
+}
+
+// Four neighbouring columns of a row of C
+__device__ __forceinline__ void i8_store4(const I8Args &a, uint32_t row, uint32_t col, uint32_t columns, i8_f32x4 v) {
+    const uint64_t at = (uint64_t)row * a.ldc + col;
+    if (a.out_kind == 0) {
+        float *const c = static_cast<float *>(a.C) + at;
+        if (a.vec) *reinterpret_cast<i8_f32x4 *>(c) = v;
+        else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (col + e < columns) c[e] = v[e];
+        }
+    } else {
+        uint16_t *const c = static_cast<uint16_t *>(a.C) + at;
+        const i8_u32x2 h = {i8_pack(a.out_kind, v[0], v[1]), i8_pack(a.out_kind, v[2], v[3])};
+        if (a.vec) *reinterpret_cast<i8_u32x2 *>(c) = h;
+        else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (col + e < columns) c[e] = (uint16_t)(h[e / 2] >> (e % 2 * 16));
+        }
+    }
+}
+
+}  // namespace ftk
