@@ -2,9 +2,9 @@
 
 Only marshals arguments.  The library must have been built (python -m
 paper_2407_21418_amd.build, or __graft_entry__.build()); a missing library is an error,
-nothing else computes in its place.  ft_plan_cached, ft_launch and ft_launch_epilogue are native
-functions (csrc/pycalls.cpp) where those were built for this interpreter, else they go through
-ctypes as all others do.
+nothing else computes in its place.  ft_plan_cached, ft_launch, ft_launch_epilogue and the calls of
+8-bit products and of tokens sorted by expert are native functions (csrc/pycalls.cpp) where those
+were built for this interpreter, else they go through ctypes as all others do.
 """
 import ctypes as C
 import importlib
@@ -15,6 +15,8 @@ try:
 except ModuleNotFoundError as e:        # not built, or for another interpreter; one that is there and does not load is an error
     if e.name != __package__ + "._pycalls":
         raise
+    _pycalls = None
+if not hasattr(_pycalls, "slow_ops"):   # built from sources that are older than this file
     _pycalls = None
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -127,6 +129,7 @@ class FtError(RuntimeError):
 
 
 _lib = None
+_NATIVE_OPS = ("ft_i8_quantize", "ft_i8_matmul", "ft_i8_matmul_experts", "ft_expert_sort", "ft_expert_gather", "ft_expert_combine", "ft_expert_combine_grad")
 
 # every symbol include/ftuner.h declares: name -> (restype, argtypes)
 _P = C.c_void_p
@@ -183,6 +186,7 @@ def lib():
             fn.restype, fn.argtypes = res, args
         if _pycalls is not None:
             _pycalls.bind(*(C.cast(fn, _P).value for fn in (l.ft_plan_cached, l.ft_launch, l.ft_launch_epilogue)))
+            _pycalls.bind_ops(*(C.cast(getattr(l, name), _P).value for name in _NATIVE_OPS))
         _lib = l
     return _lib
 
@@ -436,8 +440,11 @@ def ft_expert_combine_grad(desc: ft_expert_desc, tokens: int, dOut: int, Y: int,
     _check(lib().ft_expert_combine_grad(C.byref(desc), tokens, dOut, Y or None, row_of, weights or None, dY, dweights or None, stream), "ft_expert_combine_grad")
 
 
-# A serving loop makes these three for every Matmul: the native ones read the usual arguments themselves and hand every other call to
+# A serving loop makes these for every Matmul or layer: the native ones read the usual arguments themselves and hand every other call to
 # the functions above.
 if _pycalls is not None:
     _pycalls.slow(_check, ft_shape, CachedPlan, ft_plan_cached, ft_launch, ft_launch_epilogue)
     ft_plan_cached, ft_launch, ft_launch_epilogue = _pycalls.ft_plan_cached, _pycalls.ft_launch, _pycalls.ft_launch_epilogue
+    _pycalls.slow_ops((ft_quant_desc, ft_i8_desc, ft_i8_desc) + 4 * (ft_expert_desc,), tuple(globals()[name] for name in _NATIVE_OPS))
+    for _name in _NATIVE_OPS:
+        globals()[_name] = getattr(_pycalls, _name)

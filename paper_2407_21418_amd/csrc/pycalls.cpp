@@ -1,4 +1,5 @@
-// The calls a serving loop makes for every Matmul -- ft_plan_cached, ft_launch, ft_launch_epilogue -- as CPython functions.
+// The calls a serving loop makes for every Matmul -- ft_plan_cached, ft_launch, ft_launch_epilogue, and those of 8-bit products and of tokens
+// sorted by expert -- as CPython functions.
 //
 // Small launches take 3 to 5 us of GPU time, and a pass of shape, look-up and launch took the host 4.6 to 5.3 us: 2.3 in HIP, 0.85 in the
 // look-up's ctypes call and 0.4 around the launch's, the rest in the interpreter.  Here a call reads its arguments straight from the
@@ -89,6 +90,69 @@ PyObject *plan_cached(PyObject *, PyObject *const *a, Py_ssize_t n, PyObject *kw
     return out;
 }
 
+// The operators on device addresses: op(descriptor, numbers and addresses ..., stream = 0).  v: what stands behind the descriptor.
+typedef ft_status (*op_thunk)(void *f, const void *desc, const uint64_t *v);
+template <typename T> T *at(uint64_t v) { return reinterpret_cast<T *>(static_cast<uintptr_t>(v)); }
+ft_status quantize(void *f, const void *d, const uint64_t *v) {
+    return reinterpret_cast<decltype(&ft_i8_quantize)>(f)(static_cast<const ft_quant_desc *>(d), (uint32_t)v[0], at<const void>(v[1]), at<int8_t>(v[2]), at<float>(v[3]), at<void>(v[4]));
+}
+ft_status matmul(void *f, const void *d, const uint64_t *v) {
+    return reinterpret_cast<decltype(&ft_i8_matmul)>(f)(static_cast<const ft_i8_desc *>(d), (uint32_t)v[0], at<const int8_t>(v[1]), at<const float>(v[2]), at<const int8_t>(v[3]),
+                                                        at<const float>(v[4]), at<const float>(v[5]), at<void>(v[6]), at<void>(v[7]));
+}
+ft_status matmul_experts(void *f, const void *d, const uint64_t *v) {
+    return reinterpret_cast<decltype(&ft_i8_matmul_experts)>(f)(static_cast<const ft_i8_desc *>(d), (uint32_t)v[0], at<const int32_t>(v[1]), at<const int8_t>(v[2]), at<const float>(v[3]),
+                                                                at<const int32_t>(v[4]), (uint32_t)v[5], at<const int8_t>(v[6]), at<const float>(v[7]), at<const float>(v[8]), at<void>(v[9]),
+                                                                at<void>(v[10]));
+}
+ft_status sort(void *f, const void *d, const uint64_t *v) {
+    return reinterpret_cast<decltype(&ft_expert_sort)>(f)(static_cast<const ft_expert_desc *>(d), (uint32_t)v[0], at<const int32_t>(v[1]), at<int32_t>(v[2]), at<int32_t>(v[3]), at<int32_t>(v[4]),
+                                                          at<void>(v[5]), v[6], at<void>(v[7]));
+}
+ft_status gather(void *f, const void *d, const uint64_t *v) {
+    return reinterpret_cast<decltype(&ft_expert_gather)>(f)(static_cast<const ft_expert_desc *>(d), (uint32_t)v[0], at<const void>(v[1]), at<const int32_t>(v[2]), at<void>(v[3]), at<void>(v[4]));
+}
+ft_status combine(void *f, const void *d, const uint64_t *v) {
+    return reinterpret_cast<decltype(&ft_expert_combine)>(f)(static_cast<const ft_expert_desc *>(d), (uint32_t)v[0], at<const void>(v[1]), at<const int32_t>(v[2]), at<const float>(v[3]),
+                                                             at<void>(v[4]), at<void>(v[5]));
+}
+ft_status combine_grad(void *f, const void *d, const uint64_t *v) {
+    return reinterpret_cast<decltype(&ft_expert_combine_grad)>(f)(static_cast<const ft_expert_desc *>(d), (uint32_t)v[0], at<const void>(v[1]), at<const void>(v[2]), at<const int32_t>(v[3]),
+                                                                  at<const float>(v[4]), at<void>(v[5]), at<float>(v[6]), at<void>(v[7]));
+}
+constexpr int kOps = 7, kOpArgs = 12;
+struct Operator {
+    const char *name;
+    op_thunk call;
+    Py_ssize_t args;                     // descriptor and stream among them
+    uint32_t numbers;                    // bit i: argument i is a number, not an address
+};
+constexpr Operator kOperators[kOps] = {
+    {"ft_i8_quantize", quantize, 6, 1u << 1},  {"ft_i8_matmul", matmul, 9, 1u << 1},   {"ft_i8_matmul_experts", matmul_experts, 12, 1u << 1 | 1u << 6}, {"ft_expert_sort", sort, 9, 1u << 1 | 1u << 7},
+    {"ft_expert_gather", gather, 6, 1u << 1},  {"ft_expert_combine", combine, 7, 1u << 1}, {"ft_expert_combine_grad", combine_grad, 9, 1u << 1}};
+void *g_op[kOps];
+PyObject *g_op_desc[kOps], *g_op_slow[kOps];
+
+template <int I> PyObject *op(PyObject *, PyObject *const *a, Py_ssize_t n, PyObject *kw) {
+    constexpr Operator o = kOperators[I];
+    uint64_t v[kOpArgs] = {};
+    bool plain = g_op[I] && !kw && (n == o.args || n == o.args - 1) && (PyObject *)Py_TYPE(a[0]) == g_op_desc[I];
+    for (Py_ssize_t i = 1; plain && i < n; ++i) {
+        void *p = nullptr;
+        plain = address(a[i], &p) && !(a[i] == Py_None && (o.numbers >> i & 1u));
+        v[i - 1] = reinterpret_cast<uintptr_t>(p);
+    }
+    if (!plain) return PyObject_Vectorcall(g_op_slow[I], a, n, kw);
+    Py_buffer desc;
+    if (PyObject_GetBuffer(a[0], &desc, PyBUF_SIMPLE) != 0) return nullptr;
+    ft_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = o.call(g_op[I], desc.buf, v);
+    Py_END_ALLOW_THREADS
+    PyBuffer_Release(&desc);
+    return checked(st, o.name);
+}
+
 void keep(PyObject *&to, PyObject *from) {
     Py_INCREF(from);
     Py_XSETREF(to, from);
@@ -110,6 +174,26 @@ PyObject *bind(PyObject *, PyObject *args) {
     Py_RETURN_NONE;
 }
 
+// slow_ops(descriptor types, the ctypes functions), bind_ops(addresses in the loaded library): sequences in the order of kOperators
+PyObject *slow_ops(PyObject *, PyObject *args) {
+    PyObject *types, *functions;
+    if (!PyArg_ParseTuple(args, "O!O!", &PyTuple_Type, &types, &PyTuple_Type, &functions)) return nullptr;
+    if (PyTuple_GET_SIZE(types) != kOps || PyTuple_GET_SIZE(functions) != kOps) return PyErr_Format(PyExc_ValueError, "%d operators", kOps);
+    for (int i = 0; i < kOps; ++i) {
+        keep(g_op_desc[i], PyTuple_GET_ITEM(types, i));
+        keep(g_op_slow[i], PyTuple_GET_ITEM(functions, i));
+    }
+    Py_RETURN_NONE;
+}
+PyObject *bind_ops(PyObject *, PyObject *addresses) {
+    if (!PyTuple_Check(addresses) || PyTuple_GET_SIZE(addresses) != kOps) return PyErr_Format(PyExc_ValueError, "%d operators", kOps);
+    for (int i = 0; i < kOps; ++i) {
+        g_op[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(addresses, i));
+        if (PyErr_Occurred()) return nullptr;
+    }
+    Py_RETURN_NONE;
+}
+
 template <typename F> PyCFunction fn(F f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
 PyMethodDef methods[] = {
     {"slow", slow, METH_VARARGS, nullptr},
@@ -120,6 +204,20 @@ PyMethodDef methods[] = {
      "ft_launch(p, A, B, Cptr, stream=0)\n\nA, B, Cptr: device addresses (e.g. torch.Tensor.data_ptr()); stream: hipStream_t value."},
     {"ft_launch_epilogue", fn(launch_epilogue), METH_FASTCALL | METH_KEYWORDS,
      "ft_launch_epilogue(p, A, B, Cptr, bias, stream=0)\n\nAs ft_launch, with bias = device address of N fp32 values (0 / None for none)."},
+    {"slow_ops", slow_ops, METH_VARARGS, nullptr},
+    {"bind_ops", bind_ops, METH_VARARGS, nullptr},
+    {"ft_i8_quantize", fn(op<0>), METH_FASTCALL | METH_KEYWORDS, "ft_i8_quantize(desc, rows, X, Q, scale, stream=0)\n\nRows of values as 8-bit integers with one fp32 scale each."},
+    {"ft_i8_matmul", fn(op<1>), METH_FASTCALL | METH_KEYWORDS,
+     "ft_i8_matmul(desc, m, A, scale_a, B, scale_b, bias, Cptr, stream=0)\n\nC[i, j] = scale_a[i] * scale_b[j] * sum_k A[i, k] B[j, k] (+ bias[j]) of 8-bit integers."},
+    {"ft_i8_matmul_experts", fn(op<2>), METH_FASTCALL | METH_KEYWORDS,
+     "ft_i8_matmul_experts(desc, rows, offsets, A, scale_a, a_row, a_rows, B, scale_b, bias, Cptr, stream=0)\n\nThe same for rows sorted by expert."},
+    {"ft_expert_sort", fn(op<3>), METH_FASTCALL | METH_KEYWORDS,
+     "ft_expert_sort(desc, tokens, expert_of, offsets, row_token, row_of, workspace, workspace_bytes, stream=0)\n\nRows of the entries sorted by expert."},
+    {"ft_expert_gather", fn(op<4>), METH_FASTCALL | METH_KEYWORDS, "ft_expert_gather(desc, tokens, X, row_of, Y, stream=0)\n\nY[row_of[t, j]] = X[t]."},
+    {"ft_expert_combine", fn(op<5>), METH_FASTCALL | METH_KEYWORDS,
+     "ft_expert_combine(desc, tokens, Y, row_of, weights, Out, stream=0)\n\nOut[t] = sum_j weights[t, j] * Y[row_of[t, j]]."},
+    {"ft_expert_combine_grad", fn(op<6>), METH_FASTCALL | METH_KEYWORDS,
+     "ft_expert_combine_grad(desc, tokens, dOut, Y, row_of, weights, dY, dweights, stream=0)\n\nGradients of ft_expert_combine."},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycalls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
