@@ -27,13 +27,38 @@ struct SortArgs {
     uint32_t id_bits;                    // bits of experts - 1
 };
 
-// this wave's count of every id among its stretch [s0, s1) of the entries
-__device__ __forceinline__ void count_stretch(const SortArgs &a, uint32_t s0, uint32_t s1, uint32_t lane, uint32_t *mine) {
-    for (uint32_t i = s0 + lane; i < s1; i += 64u) {
-        const uint32_t id = (uint32_t)a.ids[i];
-        if (id < a.experts) atomicAdd(&mine[id], 1u);
+// The ids of a wave's stretch [s0, s1) of the entries, 64 at a time: the first kHeld steps are asked for together and stay in registers, so that a
+// stretch of up to 512 entries waits for memory once.  No id: ~0.
+constexpr int kHeld = 8;
+struct Stretch {
+    uint32_t s0, s1, lane, held[kHeld];
+    __device__ __forceinline__ uint32_t read(const SortArgs &a, uint32_t at) const {
+        const uint32_t id = at + lane < s1 ? (uint32_t)a.ids[at + lane] : ~0u;
+        return id < a.experts ? id : ~0u;
     }
-}
+    __device__ __forceinline__ Stretch(const SortArgs &a, uint32_t wave, uint32_t waves, uint32_t lane_) : lane(lane_) {
+        // whole steps of the block's entries, as many for each wave
+        const uint32_t b0 = blockIdx.x * a.per_block, b1 = a.n - b0 < a.per_block ? a.n : b0 + a.per_block;
+        const uint32_t steps = (b1 - b0 + 63u) / 64u, per = (steps + waves - 1u) / waves * 64u;
+        s0 = b1 - b0 < wave * per ? b1 : b0 + wave * per;
+        s1 = b1 - s0 < per ? b1 : s0 + per;
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u) held[u] = read(a, s0 + u * 64u);
+    }
+    // f(first entry, this lane's id) for every step
+    template <typename F> __device__ __forceinline__ void each(const SortArgs &a, F f) const {
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u)
+            if (s0 + u * 64u < s1) f(s0 + u * 64u, held[u]);
+        for (uint32_t at = s0 + kHeld * 64u; at < s1; at += 64u) f(at, read(a, at));
+    }
+    // counts of every id
+    __device__ __forceinline__ void count(const SortArgs &a, uint32_t *counts) const {
+        each(a, [&](uint32_t, uint32_t id) {
+            if (id != ~0u) atomicAdd(&counts[id], 1u);
+        });
+    }
+};
 // exclusive prefix sums of v[0 .. n) by one wave, in place; v[n] receives the total
 __device__ __forceinline__ void scan_by_wave(uint32_t *v, uint32_t n, uint32_t lane) {
     uint32_t carry = 0;
@@ -51,23 +76,14 @@ __device__ __forceinline__ void scan_by_wave(uint32_t *v, uint32_t n, uint32_t l
     if (lane == 0) v[n] = carry;
 }
 
-// Stretches of a block's entries: whole steps of 64, one for each wave.
-__device__ __forceinline__ void stretch_of(const SortArgs &a, uint32_t wave, uint32_t waves, uint32_t *s0, uint32_t *s1) {
-    const uint32_t b0 = blockIdx.x * a.per_block, b1 = a.n - b0 < a.per_block ? a.n : b0 + a.per_block;
-    const uint32_t steps = (b1 - b0 + 63u) / 64u, per = (steps + waves - 1u) / waves * 64u;
-    *s0 = b1 - b0 < wave * per ? b1 : b0 + wave * per;
-    *s1 = b1 - *s0 < per ? b1 : *s0 + per;
-}
-
 // counts[block][expert] of more than one block
 __global__ __launch_bounds__(1024) void ft_expert_count(SortArgs a) {
     __shared__ uint32_t lds[kMaxExperts];
     const uint32_t tid = threadIdx.x, threads = blockDim.x;
+    const Stretch stretch(a, tid / 64u, threads / 64u, tid & 63u);
     for (uint32_t e = tid; e < a.experts; e += threads) lds[e] = 0u;
     __syncthreads();
-    uint32_t s0, s1;
-    stretch_of(a, tid / 64u, threads / 64u, &s0, &s1);
-    count_stretch(a, s0, s1, tid & 63u, lds);
+    stretch.count(a, lds);
     __syncthreads();
     for (uint32_t e = tid; e < a.experts; e += threads) a.counts[(uint64_t)blockIdx.x * a.experts + e] = lds[e];
 }
@@ -77,12 +93,11 @@ __global__ __launch_bounds__(1024) void ft_expert_place(SortArgs a) {
     extern __shared__ uint32_t lds[];
     const uint32_t tid = threadIdx.x, threads = blockDim.x, lane = tid & 63u, wave = tid / 64u, waves = threads / 64u, E = a.experts;
     uint32_t *const cnt = lds, *const first = lds + waves * E, *const below = first + E + 1u, *const mine = cnt + wave * E;
+    const Stretch stretch(a, wave, waves, lane);
     for (uint32_t i = tid; i < waves * E; i += threads) cnt[i] = 0u;
     for (uint32_t e = tid; e < E; e += threads) first[e] = below[e] = 0u;
     __syncthreads();
-    uint32_t s0, s1;
-    stretch_of(a, wave, waves, &s0, &s1);
-    count_stretch(a, s0, s1, lane, mine);
+    stretch.count(a, mine);
     if (a.blocks > 1u) {
         // all blocks' counts, and those of the blocks before this one; parts of the threads take turns with the blocks
         const uint32_t parts = threads / E ? threads / E : 1u;
@@ -117,10 +132,9 @@ __global__ __launch_bounds__(1024) void ft_expert_place(SortArgs a) {
     for (uint32_t e = lane; e < E; e += 64u) mine[e] += first[e] + below[e];
     // (a wave's LDS accesses are in order: what follows touches its own counts only)
     __builtin_amdgcn_wave_barrier();
-    for (uint32_t at = s0; at < s1; at += 64u) {
+    stretch.each(a, [&](uint32_t at, uint32_t id) {
         const uint32_t i = at + lane;
-        const uint32_t id = i < s1 ? (uint32_t)a.ids[i] : ~0u;
-        const bool has = id < E;
+        const bool has = id != ~0u;
         uint64_t peers = __ballot(has);
         for (uint32_t bit = 0; bit < a.id_bits; ++bit) {
             const uint64_t set = __ballot((id >> bit) & 1u);
@@ -132,9 +146,9 @@ __global__ __launch_bounds__(1024) void ft_expert_place(SortArgs a) {
         __builtin_amdgcn_wave_barrier();
         if (has && rank == 0) mine[id] += (uint32_t)__builtin_popcountll(peers);
         __builtin_amdgcn_wave_barrier();
-        if (i < s1) a.row_of[i] = has ? (int32_t)row : -1;
+        if (i < stretch.s1) a.row_of[i] = has ? (int32_t)row : -1;
         if (has) a.row_token[row] = (int32_t)(i / a.top_k);
-    }
+    });
     // rows behind the last one
     const uint32_t used = first[E], b0 = blockIdx.x * a.per_block, b1 = a.n - b0 < a.per_block ? a.n : b0 + a.per_block;
     for (uint32_t r = b0 + tid; r < b1; r += threads)

@@ -150,7 +150,10 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
             for (int i = 0; i < BM; ++i)
 #pragma unroll
                 for (int j = 0; j < BN; ++j) acc[i][j] = i8_i32x4{0, 0, 0, 0};
-            const I8Tile next = products(g, src, ring, wave, group, lane, nk, acc, [&] { return tiles.take(g, turn); });
+            auto take = [&] { return tiles.take(g, turn); };
+            // a wave whose part of the tile lies beyond the last row or column copies for the others, and leaves them the matrix cores
+            const bool idle = (wave / GN) * WM >= tile.rows || src.cols.first + (wave % GN) * (GATED ? WN / 2 : WN) >= src.cols.of_c;
+            const I8Tile next = idle ? copies_alone(src, ring, wave, group, nk, take) : products(g, src, ring, wave, group, lane, nk, acc, take);
             const I8Tile done = tile;
             const I8Columns<TN, GATED> cols = src.cols;
             if constexpr (GK == 1) {
@@ -194,6 +197,49 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
             for (int j = 0; j < BN; ++j) kept[i][j] += sums[take + (i * BN + j) * 64u];
     }
 
+    // k-tile 0 has landed / tile t has been read by this wave and tile t + 1 has landed.  In flight beyond it: A of t + 2 (slots), or the stages up
+    // to t + STAGES - 1.  (The last results' stores may be behind the first copies: the count then waits for some of them.)
+    static __device__ __forceinline__ void first_landed(uint32_t nk) {
+        constexpr int BEHIND = SLOTS ? 2 * LA + LB : (STAGES - 1) * (LA + LB);
+        if (nk >= (uint32_t)FAR) i8_wait_copies<BEHIND>();
+        else i8_wait_copies<0>();
+        __builtin_amdgcn_s_barrier();
+    }
+    template <bool STEADY> static __device__ __forceinline__ void next_landed(uint32_t t, uint32_t nk) {
+        const uint32_t behind = nk - 1u - t;                          // tiles after t
+        if (STEADY || (SLOTS ? behind >= 2u : behind >= (uint32_t)STAGES - 1u)) i8_wait_copies<AHEAD>();
+        else i8_wait_copies<0>();
+        __builtin_amdgcn_s_barrier();
+    }
+    // the Q-th of the copies that are due once tile t has been read
+    template <int Q, bool STEADY> static __device__ __forceinline__ void copy_behind(const Source &src, unsigned char *ring, uint32_t wave, uint32_t group, uint32_t t, uint32_t nk, uint32_t sa, uint32_t sb) {
+        if constexpr (SLOTS) {
+            if constexpr (Q < LB) { if (STEADY || t + 2u < nk) src.template copy_b<Q>(ring, wave, group, t + 2u, sa); }
+            else if constexpr (STEADY) src.template copy_a<Q - LB>(ring, wave, group, t + 3u, sb);
+        } else if constexpr (STEADY) {
+            if constexpr (Q < LA) src.template copy_a<Q>(ring, wave, group, t + STAGES, sa);
+            else src.template copy_b<Q - LA>(ring, wave, group, t + STAGES, sb);
+        }
+    }
+
+    template <typename NEXT>
+    __device__ static __forceinline__ I8Tile copies_alone(const Source &src, unsigned char *ring, uint32_t wave, uint32_t group, uint32_t nk, NEXT next) {
+        uint32_t sa = 0, sb = A_BYTES, t = 0;
+        first_landed(nk);
+        for (; t + FAR < nk; ++t) {
+            next_landed<true>(t, nk);
+            i8_each<0, LA + LB>([&](auto q) { copy_behind<decltype(q)::value, true>(src, ring, wave, group, t, nk, sa, sb); });
+            sa = next_slot(sa); sb = next_slot(sb);
+        }
+        const I8Tile after = next();
+        for (; t < nk; ++t) {
+            next_landed<false>(t, nk);
+            i8_each<0, LA + LB>([&](auto q) { copy_behind<decltype(q)::value, false>(src, ring, wave, group, t, nk, sa, sb); });
+            sa = next_slot(sa); sb = next_slot(sb);
+        }
+        return after;
+    }
+
     template <typename NEXT>
     __device__ static __forceinline__ I8Tile products(const I8Args &g, const Source &src, unsigned char *ring, uint32_t wave, uint32_t group, uint32_t lane, uint32_t nk, i8_i32x4 (&acc)[BM][BN], NEXT next) {
         const uint32_t wm = wave / GN, wn = wave % GN;
@@ -202,10 +248,7 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
         const uint32_t fa = sbase + ra * 128u + (((lane >> 4) ^ i8_swizzle(ra)) << 4);
         const uint32_t fb = sbase + rb * 128u + (((lane >> 4) ^ i8_swizzle(rb)) << 4);
         uint32_t sa = 0, sb = A_BYTES;                               // slots of the tile being consumed
-        constexpr int BEHIND = SLOTS ? 2 * LA + LB : (STAGES - 1) * (LA + LB);         // copies behind k-tile 0; the last results' stores may be behind it too
-        if (nk >= (uint32_t)FAR) i8_wait_copies<BEHIND>();
-        else i8_wait_copies<0>();
-        __builtin_amdgcn_s_barrier();
+        first_landed(nk);
         Frag f0, f1;
         read_range<0, 0, NR>(fa + sa, fb + sb, f0);
         auto step = [&](uint32_t t, auto steady_c) {
@@ -229,29 +272,11 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
-            // Tile t's LDS has been read by this wave; tile t + 1 must have landed.  In flight beyond it: A of t + 2 (slots), or
-            // the stages up to t + STAGES - 1.
-            const uint32_t behind = nk - 1u - t;                      // tiles after t
-            if (STEADY || (SLOTS ? behind >= 2u : behind >= (uint32_t)STAGES - 1u)) i8_wait_copies<AHEAD>();
-            else i8_wait_copies<0>();
-            __builtin_amdgcn_s_barrier();
+            next_landed<STEADY>(t, nk);
             __builtin_amdgcn_sched_barrier(0);
             const uint32_t na = next_slot(sa), nb = next_slot(sb);
             // (past the last tile the reads fetch what happens to be there, for nobody)
-            if constexpr (SLOTS) {
-                const bool more_b = STEADY || t + 2u < nk;
-                phase<0, true>(fa + na, fb + nb, f0, f1, acc, [&](auto q) {
-                    constexpr int Q = decltype(q)::value;
-                    if constexpr (Q < LB) { if (more_b) src.template copy_b<Q>(ring, wave, group, t + 2u, sa); }
-                    else if constexpr (STEADY) src.template copy_a<Q - LB>(ring, wave, group, t + 3u, sb);
-                });
-            } else {
-                phase<0, STEADY>(fa + na, fb + nb, f0, f1, acc, [&](auto q) {
-                    constexpr int Q = decltype(q)::value;
-                    if constexpr (Q < LA) src.template copy_a<Q>(ring, wave, group, t + STAGES, sa);
-                    else src.template copy_b<Q - LA>(ring, wave, group, t + STAGES, sb);
-                });
-            }
+            phase<0, SLOTS || STEADY>(fa + na, fb + nb, f0, f1, acc, [&](auto q) { copy_behind<decltype(q)::value, STEADY>(src, ring, wave, group, t, nk, sa, sb); });
             sa = na; sb = nb;
         };
         uint32_t t = 0;

@@ -21,94 +21,74 @@
 
 namespace ftk {
 
-// Few rows: tiles of 16 MB x 16 NB whose W waves take turns along the reduce axis, 128 bytes of it at a time, straight from memory into the
-// matrix cores' operands; their sums meet in LDS.  Every byte of either operand is loaded by one wave of a workgroup once.
-template <int MB, int NB, int W, int AHEAD, bool GROUPED, bool GATED> __global__ __launch_bounds__(W * 64) void ft_i8_stream(I8Args a) {
-    static_assert(!GATED || NB % 2 == 0, "gates and values in pairs");
-    __shared__ i8_i32x4 sums[W * MB * NB * 64];
-    constexpr int TM = MB * 16, TN = NB * 16;
+// Few rows: tiles of 16 rows by 16 columns (by 16 gates and their values) whose eight waves take turns along the reduce axis, 128 bytes of it
+// at a time, straight from memory into the matrix cores' operands, AHEAD turns under way; their sums meet in LDS.  Every byte of either
+// operand is loaded by one wave of a workgroup once.  What the sums are scaled with is asked for before the products.
+template <int AHEAD, bool GROUPED, bool GATED> __global__ __launch_bounds__(512) void ft_i8_stream(I8Args a) {
+    constexpr int W = 8, NB = GATED ? 2 : 1;
+    __shared__ i8_i32x4 sums[W][NB][64];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u);
-    const I8Tile t = I8Tiles<TM, TN, GROUPED>(a).take(a, 0);
+    const I8Tile t = I8Tiles<16, 16 * NB, GROUPED>(a).take(a, 0);
     if (!t.some) return;
-    const __amdgpu_buffer_rsrc_t ar = GROUPED ? i8_rsrc(a.A, a.a_rows * a.lda) : i8_rsrc(a.A + (uint64_t)t.row0 * a.lda, t.rows * a.lda);
-    const I8Columns<TN, GATED> cols(a, t);
-    const uint32_t kc = (lane >> 4) * 16u;
-    uint32_t off_a[MB], off_b[NB];
-#pragma unroll
-    for (int i = 0; i < MB; ++i) {
-        const uint32_t r = i * 16u + (lane & 15u);
-        if constexpr (GROUPED) {
-            const uint32_t s = r < t.rows ? i8_source<true>(a, t.row0 + r) : ~0u;
-            off_a[i] = s == ~0u ? kOutside : s * a.lda + kc;
-        } else off_a[i] = r * a.lda + kc;
-    }
-#pragma unroll
-    for (int j = 0; j < NB; ++j) off_b[j] = (cols.row_of_block(j) + (lane & 15u)) * a.ldb + kc;
-    i8_i32x4 acc[MB][NB];
-#pragma unroll
-    for (int i = 0; i < MB; ++i)
-#pragma unroll
-        for (int j = 0; j < NB; ++j) acc[i][j] = i8_i32x4{0, 0, 0, 0};
-
-    struct Step { i8_u32x4 a[2][MB], b[2][NB]; };
-    auto load = [&](uint32_t s, Step &f) {                   // (beyond the reduce axis: zeros)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t k = s * 128u + h * 64u;
-            const bool in = k + kc < a.k;
-#pragma unroll
-            for (int j = 0; j < NB; ++j) f.b[h][j] = i8_load(cols.operand(j), in ? off_b[j] + k : kOutside);
-#pragma unroll
-            for (int i = 0; i < MB; ++i) f.a[h][i] = i8_load(ar, in ? off_a[i] + k : kOutside);
-        }
-    };
-    auto use = [&](uint32_t s, Step &f) {
-        if (s * 128u + 128u > a.k) {                         // the last step's rows end inside
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < MB; ++i) f.a[h][i] = i8_cut(f.a[h][i], s * 128u + h * 64u + kc, a.k);
-        }
+    const I8Columns<16 * NB, GATED> cols(a, t);
+    const uint32_t kc = (lane >> 4) * 16u, r = lane & 15u, steps = (a.k + 127u) / 128u, off_b = r * a.ldb + kc;
+    const uint32_t source = r < t.rows ? i8_source<GROUPED>(a, t.row0 + r) : ~0u;
+    struct Step { i8_u32x4 a[2], b[2][NB]; };
+    Step f[AHEAD];
+    auto load_b = [&](uint32_t s, Step &f) {                 // (beyond the reduce axis: zeros)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < MB; ++i)
-#pragma unroll
-                for (int j = 0; j < NB; ++j) acc[i][j] = i8_mfma(f.b[h][j], f.a[h][i], acc[i][j]);
+            for (int j = 0; j < NB; ++j) f.b[h][j] = i8_load(cols.operand(j), s * 128u + h * 64u + kc < a.k ? off_b + s * 128u + h * 64u : kOutside);
     };
-    const uint32_t steps = (a.k + 127u) / 128u;
-    Step f[AHEAD];
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) load(wave + i * W, f[i]);
+    for (int i = 0; i < AHEAD; ++i) load_b(wave + i * W, f[i]);
+    const __amdgpu_buffer_rsrc_t ar = GROUPED ? i8_rsrc(a.A, a.a_rows * a.lda) : i8_rsrc(a.A + (uint64_t)t.row0 * a.lda, t.rows * a.lda);
+    const uint32_t off_a = GROUPED ? (source == ~0u ? kOutside : source * a.lda + kc) : r * a.lda + kc;
+    auto load_a = [&](uint32_t s, Step &f) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) f.a[h] = i8_load(ar, s * 128u + h * 64u + kc < a.k ? off_a + s * 128u + h * 64u : kOutside);
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) load_a(wave + i * W, f[i]);
+    // wave 0 has the tile's results: row r, four columns from `col`
+    const uint32_t col = cols.first + (lane >> 4) * 4u;
+    const bool mine = wave == 0 && r < t.rows && col < cols.of_c;
+    I8Scales<GATED> scales;
+    float sa = 0.f;
+    if (mine) {
+        scales.load(cols, a, t, col);
+        if (source != ~0u) sa = a.scale_a[source];
+    }
+    i8_i32x4 acc[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[j] = i8_i32x4{0, 0, 0, 0};
     for (uint32_t s = wave; s < steps; s += AHEAD * W) {
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            use(s + i * W, f[i]);                            // (beyond the last step: zeros)
-            load(s + (i + AHEAD) * W, f[i]);
+            const uint32_t now = s + i * W;                  // (beyond the last step: zeros)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (now * 128u + 128u > a.k) f[i].a[h] = i8_cut(f[i].a[h], now * 128u + h * 64u + kc, a.k);      // rows end inside the last step
+#pragma unroll
+                for (int j = 0; j < NB; ++j) acc[j] = i8_mfma(f[i].b[h][j], f[i].a[h], acc[j]);
+            }
+            if (now + AHEAD * W < steps) {
+                load_b(now + AHEAD * W, f[i]);
+                load_a(now + AHEAD * W, f[i]);
+            }
         }
     }
 #pragma unroll
-    for (int i = 0; i < MB; ++i)
-#pragma unroll
-        for (int j = 0; j < NB; ++j) sums[(wave * (MB * NB) + i * NB + j) * 64u + lane] = acc[i][j];
+    for (int j = 0; j < NB; ++j) sums[wave][j][lane] = acc[j];
     __syncthreads();
-    constexpr int NP = GATED ? NB / 2 : NB;                  // blocks of columns of C
-    for (uint32_t item = threadIdx.x; item < MB * NP * 64u; item += W * 64u) {
-        const uint32_t l = item & 63u, j = item / 64u % NP, i = item / 64u / NP, r = i * 16u + (l & 15u), col = cols.first + j * 16u + (l >> 4) * 4u;
-        if (r >= t.rows || col >= cols.of_c) continue;
-        auto sum = [&](uint32_t block) {
-            i8_i32x4 v = sums[(i * NB + block) * 64u + l];
+    if (!mine) return;
 #pragma unroll
-            for (int w = 1; w < W; ++w) v += sums[(w * (MB * NB) + i * NB + block) * 64u + l];
-            return v;
-        };
-        const uint32_t s = i8_source<GROUPED>(a, t.row0 + r);
-        const float sa = s == ~0u ? 0.f : a.scale_a[s];
-        I8Scales<GATED> scales;
-        scales.load(cols, a, t, col);
-        if constexpr (GATED) i8_store4(a, t.row0 + r, col, cols.of_c, i8_gated(scales, sa, sum(2u * j), sum(2u * j + 1u)));
-        else i8_store4(a, t.row0 + r, col, cols.of_c, i8_scaled(scales, sa, sum(j)));
-    }
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int w = 1; w < W; ++w) acc[j] += sums[w][j][lane];
+    if constexpr (GATED) i8_store4(a, t.row0 + r, col, cols.of_c, i8_gated(scales, sa, acc[0], acc[1]));
+    else i8_store4(a, t.row0 + r, col, cols.of_c, i8_scaled(scales, sa, acc[0]));
 }
 
 }  // namespace ftk
@@ -117,9 +97,9 @@ using namespace ftk;
 
 namespace {
 
-template <int MB, int NB, int W, int AHEAD, bool GROUPED, bool GATED> ft_status launch_stream(I8Args &a, hipStream_t s) {
-    if (!i8_grid(a, MB * 16, NB * 16, GROUPED)) return FT_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((ft_i8_stream<MB, NB, W, AHEAD, GROUPED, GATED>), dim3(a.row_tiles * a.col_tiles), dim3(W * 64), 0, s, a);
+template <bool GROUPED, bool GATED> ft_status launch_stream(I8Args &a, hipStream_t s) {
+    if (!i8_grid(a, 16, GATED ? 32 : 16, GROUPED)) return FT_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((ft_i8_stream<2, GROUPED, GATED>), dim3(a.row_tiles * a.col_tiles), dim3(512), 0, s, a);
     return op_launched();
 }
 // compute units of the current device
@@ -141,7 +121,7 @@ template <bool GROUPED> ft_status run(I8Args &a, void *stream) {
     const I8Kind kind = i8_choose(a, GROUPED);
     if (kind != I8_STREAM) return i8_launch_blocks(kind, GROUPED, a, stream);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return a.gated ? launch_stream<1, 2, 8, 2, GROUPED, true>(a, s) : launch_stream<1, 1, 8, 2, GROUPED, false>(a, s);
+    return a.gated ? launch_stream<GROUPED, true>(a, s) : launch_stream<GROUPED, false>(a, s);
 }
 
 }  // namespace

@@ -88,7 +88,7 @@ inline ft_status i8_check(const ft_i8_desc *d, bool grouped, uint32_t m, const i
 
 // ---- tokens by expert ----
 // The sort: up to kSortOne entries in one workgroup; more in at most kSortBlocks blocks, whose counts for each expert are the workspace.
-constexpr uint32_t kSortOne = 8192, kSortBlock = 4096, kSortBlocks = 256;
+constexpr uint32_t kSortOne = 8192, kSortBlock = 2048, kSortBlocks = 256;
 inline uint32_t sort_blocks(uint64_t entries) {
     if (entries <= kSortOne) return 1u;
     const uint64_t blocks = (entries + kSortBlock - 1) / kSortBlock;

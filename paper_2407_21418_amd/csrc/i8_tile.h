@@ -141,7 +141,6 @@ template <int TN, bool GATED> struct I8Columns {
         b = i8_rsrc(w + (uint64_t)first * a.ldb, rows * a.ldb);
         values = GATED ? i8_rsrc(w + (uint64_t)(of_c + first) * a.ldb, rows * a.ldb) : b;
     }
-    __device__ __forceinline__ uint32_t row_of_block(int j) const { return (GATED ? j / 2 : j) * 16u; }
     __device__ __forceinline__ __amdgpu_buffer_rsrc_t operand(int j) const { return GATED && j % 2 ? values : b; }
 };
 // four neighbouring values of a vector of `n`, at any alignment; beyond its end the first of them again
