@@ -87,12 +87,12 @@ inline ft_status i8_check(const ft_i8_desc *d, bool grouped, uint32_t m, const i
 }
 
 // ---- tokens by expert ----
-// The sort: up to kSortOne entries in one workgroup; more in at most kSortBlocks blocks, whose counts for each expert are the workspace.
-constexpr uint32_t kSortOne = 8192, kSortBlock = 2048, kSortBlocks = 256;
+// The sort: blocks of 1024 entries, each of which counts all entries itself, up to kSortRecount of them; beyond, at most kSortBlocks blocks,
+// whose counts for each expert are the workspace of a launch before.
+constexpr uint32_t kSortRecount = 16384, kSortSmall = 1024, kSortBlock = 2048, kSortBlocks = 256;
 inline uint32_t sort_blocks(uint64_t entries) {
-    if (entries <= kSortOne) return 1u;
-    const uint64_t blocks = (entries + kSortBlock - 1) / kSortBlock;
-    return blocks < kSortBlocks ? (uint32_t)blocks : kSortBlocks;
+    const uint64_t blocks = entries <= kSortRecount ? (entries + kSortSmall - 1) / kSortSmall : (entries + kSortBlock - 1) / kSortBlock;
+    return blocks < 1 ? 1u : blocks < kSortBlocks ? (uint32_t)blocks : kSortBlocks;
 }
 
 inline ft_status expert_shape(const ft_expert_desc *d, uint32_t tokens) {
@@ -104,8 +104,8 @@ inline ft_status expert_workspace(const ft_expert_desc *d, uint32_t tokens, uint
     if (!bytes) return FT_ERR_INVALID_ARG;
     const ft_status st = expert_shape(d, tokens);
     if (st != FT_OK) return st;
-    const uint32_t blocks = sort_blocks((uint64_t)tokens * d->top_k);
-    *bytes = blocks > 1 ? (uint64_t)blocks * d->experts * 4u : 0u;
+    const uint64_t entries = (uint64_t)tokens * d->top_k;
+    *bytes = entries > kSortRecount ? (uint64_t)sort_blocks(entries) * d->experts * 4u : 0u;
     return FT_OK;
 }
 inline ft_status sort_check(const ft_expert_desc *d, uint32_t tokens, const int32_t *expert_of, int32_t *offsets, int32_t *row_token, int32_t *row_of, void *workspace,

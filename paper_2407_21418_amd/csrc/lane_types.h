@@ -7,9 +7,7 @@ namespace ftk {
 
 // gfx950 loads and stores 16 bytes at any address that is aligned to the elements: rows of any pitch take one path
 typedef uint32_t row_u32x4 __attribute__((ext_vector_type(4)));
-struct __attribute__((packed, aligned(2))) RowPiece {
-    row_u32x4 v;
-};
+typedef uint32_t RowPiece __attribute__((ext_vector_type(4), aligned(2)));
 
 typedef float row_f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 row_bf16x2 __attribute__((ext_vector_type(2)));
@@ -45,8 +43,12 @@ template <int DT> struct RowType {
         return v;
     }
     // piece of a row at p, of which n >= 1 elements are the row's; the others read as zeros
-    static __device__ __forceinline__ row_u32x4 load(const unsigned char *p, uint32_t n) {
-        if (n >= (uint32_t)V) return reinterpret_cast<const RowPiece *>(p)->v;
+    // STREAM: what is not asked for again is not kept in the caches
+    template <bool STREAM = false> static __device__ __forceinline__ row_u32x4 load(const unsigned char *p, uint32_t n) {
+        if (n >= (uint32_t)V) {
+            if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const RowPiece *>(p));
+            else return *reinterpret_cast<const RowPiece *>(p);
+        }
         row_u32x4 v = {0u, 0u, 0u, 0u};
 #pragma unroll
         for (int i = 0; i < V - 1; ++i) {
@@ -56,9 +58,10 @@ template <int DT> struct RowType {
         }
         return v;
     }
-    static __device__ __forceinline__ void store(unsigned char *p, row_u32x4 v, uint32_t n) {
+    template <bool STREAM = false> static __device__ __forceinline__ void store(unsigned char *p, row_u32x4 v, uint32_t n) {
         if (n >= (uint32_t)V) {
-            reinterpret_cast<RowPiece *>(p)->v = v;
+            if constexpr (STREAM) __builtin_nontemporal_store((RowPiece)v, reinterpret_cast<RowPiece *>(p));
+            else *reinterpret_cast<RowPiece *>(p) = v;
             return;
         }
 #pragma unroll
