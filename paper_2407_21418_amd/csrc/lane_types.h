@@ -73,7 +73,8 @@ template <int DT> struct RowType {
     }
 };
 
-// g / (1 + exp(-g)) * u; of a gate far below zero a zero
-__device__ __forceinline__ float silu_mul(float g, float u) { return g * __builtin_amdgcn_rcpf(1.f + expf(-g)) * u; }
+// g / (1 + exp(-g)) * u.  exp(-g) is 2^(-g log2 e) with the exponent rounded: within (1.22 |g| + 2) 2^-24 of itself, which a gate far below zero, whose
+// result is next to nothing, feels most; a third of the instructions of a call of expf, and infinities and NaNs come out as by the formula.
+__device__ __forceinline__ float silu_mul(float g, float u) { return g * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-0x1.715476p+0f * g)) * u; }
 
 }  // namespace ftk

@@ -3,11 +3,11 @@
 // Bound by memory: a row is read once, stays in its threads' registers while its largest magnitude is found, and
 // leaves as integers.  Rows of more than 32768 columns are read a second time.
 //
-// scale = amax / 127 and q = 127 f / amax to nearest even.  For 16-bit f this is exact without a division for each value: t = f *
-// (127 / amax) is off by at most 2^-23 of itself.  127 f / amax lies exactly in the middle between two integers or at
-// least 2^-19 of itself away from there (f = a 2^p, amax = d 2^q with a, d < 2^11 make 254 a 2^p - odd d 2^q a multiple of 2^p, and
-// 2^p / (2 d 2^q) over 127 a 2^p / (d 2^q) is more than 2^-19).  So t rounded to 21 bits -- the middles have at most 9 -- rounds
-// to the integer that the exact quotient rounds to.
+// scale = amax / 127 and q = 127 f / amax to nearest even.  For 16-bit f this is exact without a division for each value: with 127 / amax
+// as the sum of two fp32, t = f * hi + f * lo is the quotient rounded once, 2^-24 of itself.  127 f / amax lies exactly in the middle
+// between two integers, and then t is that middle, or at least 2^-19 of itself away from there (f = a 2^p, amax = d 2^q with a,
+// d < 2^11 make 254 a 2^p - odd d 2^q a multiple of 2^p, and 2^p / (2 d 2^q) over 127 a 2^p / (d 2^q) is more than 2^-19): t rounds to
+// the integer that the quotient rounds to.  Adding 1.5 * 2^23 does that and leaves the integer in the low byte.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -17,14 +17,6 @@
 #include "op_launch.h"
 
 namespace ftk {
-
-// t to 21 bits (Veltkamp's splitting; t <= 127)
-__device__ __forceinline__ float to_21_bits(float t) {
-#pragma clang fp contract(off)
-    const float c = t * 9.f;
-    const float d = c - t;
-    return c - d;
-}
 
 // The values of a piece of 8 columns, zeros beyond the row's end
 template <int DT, bool GATED> struct QuantPiece {
@@ -78,30 +70,37 @@ __device__ __forceinline__ uint32_t largest(const float (&f)[8], uint32_t m) {
     return m;
 }
 
+// Rows of very small or large values are multiplied with a power of two first, so that 127 / amax and what it leaves are normal.
 struct RowScale {
-    float up, per;                       // q = f * up * per; rows of tiny values are lifted so that 127 / amax is finite
-    float scale;
-};
-__device__ __forceinline__ RowScale row_scale(uint32_t bits) {
-    RowScale r = {1.f, 0.f, 0.f};
-    if (bits >= 0x7f800000u) r.scale = __builtin_nanf("");
-    else if (bits != 0) {
+    float lift, hi, lo, scale;
+    bool fine;
+    __device__ __forceinline__ explicit RowScale(uint32_t bits) : lift(1.f), hi(0.f), lo(0.f), scale(0.f), fine(bits < 0x7f800000u) {
         const float amax = __builtin_bit_cast(float, bits);
-        if (amax < 0x1p-100f) r.up = 0x1p100f;
-        r.per = 127.f / (amax * r.up);
-        r.scale = amax / 127.f;
+        if (!fine) scale = __builtin_nanf("");
+        else if (bits != 0) {
+            if (amax < 0x1p-60f) lift = 0x1p100f;
+            else if (amax > 0x1p60f) lift = 0x1p-60f;
+            const float peak = amax * lift;
+            hi = 127.f / peak;
+            lo = __builtin_fmaf(-hi, peak, 127.f) / peak;
+            scale = amax / 127.f;
+        }
     }
-    return r;
-}
-__device__ __forceinline__ uint2 integers(const float (&f)[8], const RowScale &r, bool fine) {
-    uint32_t w[2] = {0u, 0u};
+    __device__ __forceinline__ uint2 integers(float (&f)[8]) const {
+        if (!fine) return make_uint2(0u, 0u);
+        if (lift != 1.f) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int q = fine ? (int)__builtin_rintf(to_21_bits(f[i] * r.up * r.per)) : 0;
-        w[i / 4] |= ((uint32_t)q & 255u) << (i % 4 * 8);
+            for (int i = 0; i < 8; ++i) f[i] *= lift;
+        }
+        uint32_t q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = __builtin_bit_cast(uint32_t, __builtin_fmaf(f[i], hi, f[i] * lo) + 0x1.8p23f);
+        return make_uint2(low_bytes(q[0], q[1], q[2], q[3]), low_bytes(q[4], q[5], q[6], q[7]));
     }
-    return make_uint2(w[0], w[1]);
-}
+    static __device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+        return __builtin_amdgcn_perm(b, a, 0x0c0c0400u) | __builtin_amdgcn_perm(d, c, 0x04000c0cu);
+    }
+};
 
 // `threads` threads for a row: 64, four rows to a workgroup, or a whole workgroup.  HELD: pieces that a thread keeps; 0: as many as
 // there are, read twice
@@ -147,19 +146,18 @@ template <int DT, bool GATED, int HELD> __global__ __launch_bounds__(1024) void 
         __syncthreads();
         for (uint32_t w = 0; w < threads / 64u; ++w) m = most[w] > m ? most[w] : m;
     }
-    const bool fine = m < 0x7f800000u;
-    const RowScale s = row_scale(m);
+    const RowScale s(m);
     if (tid == 0) a.scale[r] = s.scale;
     if constexpr (HELD > 0) {
 #pragma unroll
         for (int i = 0; i < H; ++i)
-            if (tid + i * threads < pieces) *reinterpret_cast<uint2 *>(out + (tid + i * threads) * 8u) = integers(f[i], s, fine);
+            if (tid + i * threads < pieces) *reinterpret_cast<uint2 *>(out + (tid + i * threads) * 8u) = s.integers(f[i]);
     } else {
         for (uint32_t p = tid; p < pieces; p += threads) {
             typename P::Raw x;
             P::load(a, row, p, x);
             P::values(x, f[0]);
-            *reinterpret_cast<uint2 *>(out + p * 8u) = integers(f[0], s, fine);
+            *reinterpret_cast<uint2 *>(out + p * 8u) = s.integers(f[0]);
         }
     }
     for (uint32_t p = pieces + tid; p < a.ldq / 8u; p += threads) *reinterpret_cast<uint2 *>(out + p * 8u) = make_uint2(0u, 0u);

@@ -82,7 +82,7 @@ class Layer:
             assert bool(((self.h[rows].double() - f).abs() <= bound).all())
             f = self.h[rows].double()
             peak = f.abs().amax(1, keepdim=True)
-            assert bool(((self.qh[rows, :self.ffn].double() - 127 * f / peak).abs() <= 0.5 + 127 * 3.5 * 2.0 ** -23).all())
+            assert bool(((self.qh[rows, :self.ffn].double() - 127 * f / peak).abs() <= 0.5 + 127 * 2.0 ** -23).all())
             assert torch.equal(self.sh[rows], (peak[:, 0] / 127).float())
             ref = product(self.qh[rows], self.sh[rows], self.w2, self.s2, self.cols, self.ffn, e)
             assert bool(((self.y[rows].double() - ref).abs() <= (2.0 ** -8 * 1.0001 + 4.01 * 2.0 ** -24) * ref.abs() + 2.0 ** -134).all())
