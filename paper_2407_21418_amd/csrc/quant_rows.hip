@@ -170,9 +170,12 @@ using namespace ftk;
 namespace {
 
 template <int DT, bool GATED> void launch(const QuantArgs &a, hipStream_t s) {
-    // two pieces a thread where the row has that many
+    // Pieces of a thread: one where a few rows leave the device idle (16 x 4096 bf16 3.0 us, with two 3.25; from 1024 rows on alike), four where
+    // more in flight is what wide rows lack (8192 x 4096 bf16 20.8 us, with two 22.1; 8192 x 11008 48.9 and 50.9), else two (65536 x 1408 fp32
+    // 81.0 us, with four 83.2; 2048 x 2 x 11008 gated 24.0 and 25.8; 8192 x 2048 bf16 12.7 and 13.6).
     const uint32_t pieces = (a.cols + 7u) / 8u;
-    uint32_t threads = ((pieces + 1u) / 2u + 63u) / 64u * 64u;
+    const uint32_t hold = a.rows <= 256u ? 1u : !GATED && DT != ROW_F32 && a.cols >= 4096u ? 4u : 2u;
+    uint32_t threads = ((pieces + hold - 1u) / hold + 63u) / 64u * 64u;
     if (threads > 1024u) threads = 1024u;
     const uint32_t per = threads == 64u ? 4u : 1u;
     const dim3 grid((a.rows + per - 1u) / per), block(threads * per);
