@@ -134,6 +134,32 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
         }
     }
 
+    static constexpr int PER = GATED ? 2 : 1, NP = BN / PER;         // blocks of columns of C that a wave has
+    // Where a wave's results lie -- lane l holds row l % 16, columns 4 * (l / 16) .. + 3 of every 16 x 16 block -- and what they are scaled with
+    struct Finals {
+        uint32_t r0, c0, source[KEEP];
+        float sr[KEEP];
+        I8Scales<GATED> scales[NP];
+        __device__ __forceinline__ void ask(const I8Args &g, const I8Tile &tile, const I8Columns<TN, GATED> &cols, uint32_t wave, uint32_t group, uint32_t lane) {
+            r0 = (wave / GN) * WM + group * (KEEP * 16) + (lane & 15u);
+            c0 = cols.first + (wave % GN) * (WN / PER) + (lane >> 4) * 4u;
+#pragma unroll
+            for (int i = 0; i < KEEP; ++i) source[i] = r0 + i * 16u < tile.rows ? i8_source<GROUPED>(g, tile.row0 + r0 + i * 16u) : ~0u;
+#pragma unroll
+            for (int j = 0; j < NP; ++j) {
+                const uint32_t col = c0 + j * 16u;
+                scales[j].load(cols, g, tile, col < cols.of_c ? col : cols.of_c - 1u);
+            }
+        }
+        __device__ __forceinline__ void rows(const I8Args &g) {
+#pragma unroll
+            for (int i = 0; i < KEEP; ++i) sr[i] = source[i] == ~0u ? 0.f : g.scale_a[source[i]];
+        }
+    };
+    // Small waves ask for their scales before the products (128 x 4096 x 4096 9.9 -> 9.55 us, 1024 x 2304 x 768 8.35 -> 8.1); large ones have no
+    // registers for that, and by expert the copies would wait behind two reads in a row (16 experts of 125 rows 15.8 -> 16.6).
+    static constexpr bool EARLY = BM * BN <= 8 && !GROUPED;
+
     // All tiles of a workgroup.  The ring is filled for the next one while the last one's sums are scaled and stored.
     __device__ static __forceinline__ void run(const I8Args &g, unsigned char *smem) {
         const uint32_t tid = threadIdx.x, lane = tid & 63u, all = __builtin_amdgcn_readfirstlane(tid >> 6), wave = GK > 1 ? all % NW : all, group = GK > 1 ? all / NW : 0u;
@@ -143,7 +169,10 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
         I8Tile tile = tiles.take(g, 0);
         if (!tile.some) return;
         Source src(g, tile, wave, lane);
+        Finals fin;
+        if constexpr (EARLY) fin.ask(g, tile, src.cols, wave, group, lane);
         fill(src, ring, wave, group, nk);
+        if constexpr (EARLY) fin.rows(g);
         for (uint32_t turn = 1;; ++turn) {
             i8_i32x4 acc[BM][BN];
 #pragma unroll
@@ -152,29 +181,30 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
                 for (int j = 0; j < BN; ++j) acc[i][j] = i8_i32x4{0, 0, 0, 0};
             auto take = [&] { return tiles.take(g, turn); };
             // a wave whose part of the tile lies beyond the last row or column copies for the others, and leaves them the matrix cores
-            const bool idle = (wave / GN) * WM >= tile.rows || src.cols.first + (wave % GN) * (GATED ? WN / 2 : WN) >= src.cols.of_c;
+            const bool idle = (wave / GN) * WM >= tile.rows || src.cols.first + (wave % GN) * (WN / PER) >= src.cols.of_c;
             const I8Tile next = idle ? copies_alone(src, ring, wave, group, nk, take) : products(g, src, ring, wave, group, lane, nk, acc, take);
             const I8Tile done = tile;
             const I8Columns<TN, GATED> cols = src.cols;
-            if constexpr (GK == 1) {
-                if (next.some) {
-                    // (every wave has read the last k-tile: they met after its second k-step had arrived)
-                    src = Source(g, next, wave, lane);
-                    fill(src, ring, wave, group, nk);
-                }
-                results(g, done, cols, (wave / GN) * WM, wave % GN, lane, acc);
-            } else {
-                i8_i32x4 kept[KEEP][BN];
-                meet(smem, wave, group, lane, acc, kept);
-                if (next.some) {
-                    __syncthreads();                                 // the sums have been read
-                    src = Source(g, next, wave, lane);
-                    fill(src, ring, wave, group, nk);
-                }
-                results(g, done, cols, (wave / GN) * WM + group * (KEEP * 16), wave % GN, lane, kept);
+            i8_i32x4 kept[KEEP][BN];
+            if constexpr (GK > 1) meet(smem, wave, group, lane, acc, kept);
+            if constexpr (!EARLY) {
+                fin.ask(g, done, cols, wave, group, lane);
+                fin.rows(g);
             }
+            if (next.some) {
+                // (every wave has read the last k-tile: they met after its second k-step had arrived)
+                if constexpr (GK > 1) __syncthreads();               // the sums have been read
+                src = Source(g, next, wave, lane);
+                fill(src, ring, wave, group, nk);
+            }
+            if constexpr (GK > 1) results(g, done, cols, fin, lane, kept);
+            else results(g, done, cols, fin, lane, acc);
             if (!next.some) return;
             tile = next;
+            if constexpr (EARLY) {
+                fin.ask(g, tile, src.cols, wave, group, lane);
+                fin.rows(g);
+            }
         }
     }
 
@@ -287,36 +317,21 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
         return after;
     }
 
-    // Sums to C: lane l holds row l % 16, columns 4 * (l / 16) .. + 3 of every 16 x 16 block, the first at row `row`, wave column wn
-    template <int NI>
-    __device__ static __forceinline__ void results(const I8Args &g, const I8Tile &tile, const I8Columns<TN, GATED> &cols, uint32_t row, uint32_t wn, uint32_t lane, const i8_i32x4 (&acc)[NI][BN]) {
-        const uint32_t r0 = row + (lane & 15u), q4 = lane >> 4;
-        float sr[NI];
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            const uint32_t r = r0 + i * 16u, s = r < tile.rows ? i8_source<GROUPED>(g, tile.row0 + r) : ~0u;
-            sr[i] = s == ~0u ? 0.f : g.scale_a[s];
-        }
-        constexpr int PER = GATED ? 2 : 1, NP = BN / PER;             // blocks of columns of C
-        const uint32_t c0 = cols.first + wn * (WN / PER) + q4 * 4u;
-        I8Scales<GATED> scales[NP];
-#pragma unroll
-        for (int j = 0; j < NP; ++j) {
-            const uint32_t col = c0 + j * 16u;
-            scales[j].load(cols, g, tile, col < cols.of_c ? col : cols.of_c - 1u);
-        }
+    // Sums to C
+    __device__ static __forceinline__ void results(const I8Args &g, const I8Tile &tile, const I8Columns<TN, GATED> &cols, const Finals &fin, uint32_t lane, const i8_i32x4 (&acc)[KEEP][BN]) {
+        const uint32_t r0 = fin.r0, c0 = fin.c0, q4 = lane >> 4;
         auto value = [&](int i, int j) -> i8_f32x4 {
-            if constexpr (GATED) return i8_gated(scales[j], sr[i], acc[i][2 * j], acc[i][2 * j + 1]);
-            else return i8_scaled(scales[j], sr[i], acc[i][j]);
+            if constexpr (GATED) return i8_gated(fin.scales[j], fin.sr[i], acc[i][2 * j], acc[i][2 * j + 1]);
+            else return i8_scaled(fin.scales[j], fin.sr[i], acc[i][j]);
         };
         bool pairs = false;
         if constexpr (NP % 2 == 0) pairs = g.vec && g.out_kind != 0;
         if (pairs) {
             // two neighbouring blocks: after the swap of odd and even 16-lane rows a lane holds 8 columns of one of them
             uint16_t *const C = static_cast<uint16_t *>(g.C);
-            const uint32_t cc = cols.first + wn * (WN / PER) + (q4 & 1u) * 16u + (q4 >> 1) * 8u;
+            const uint32_t cc = c0 - q4 * 4u + (q4 & 1u) * 16u + (q4 >> 1) * 8u;
 #pragma unroll
-            for (int i = 0; i < NI; ++i)
+            for (int i = 0; i < KEEP; ++i)
 #pragma unroll
                 for (int j = 0; j + 1 < NP; j += 2) {
                     const i8_f32x4 x = value(i, j), y = value(i, j + 1);
@@ -328,7 +343,7 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
                 }
         } else {
 #pragma unroll
-            for (int i = 0; i < NI; ++i)
+            for (int i = 0; i < KEEP; ++i)
 #pragma unroll
                 for (int j = 0; j < NP; ++j) {
                     const uint32_t r = r0 + i * 16u, col = c0 + j * 16u;
