@@ -86,6 +86,19 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
         if constexpr (M + 1 < NM) phase<KS, COPY, M + 1>(aa, ba, fill, use, acc, copy);
     }
 
+    // By expert: the rows of A that this lane's copies of a tile take, asked for a tile ahead
+    struct CopyRows {
+        uint32_t of_a[GROUPED ? LA : 1];
+        __device__ __forceinline__ void ask(const I8Args &g, const I8Tile &tile, uint32_t wave, uint32_t lane) {
+            if constexpr (GROUPED) {
+#pragma unroll
+                for (int i = 0; i < LA; ++i) {
+                    const uint32_t row = wave * (LA * 8) + i * 8 + lane / 8u;
+                    of_a[i] = row < tile.rows ? i8_source<true>(g, tile.row0 + row) : ~0u;
+                }
+            }
+        }
+    };
     // Where a tile's operands lie.  Copies: wave instruction i fills 1 KB, eight rows, of the tile.  A row that is not there, and what lies beyond the
     // last one, reads as zeros by the buffer's bound; bytes beyond K are whatever follows, and are cut from A's fragments.
     struct Source {
@@ -93,15 +106,13 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
         I8Columns<TN, GATED> cols;
         uint32_t off_a[LA], off_b[LB];
         // (wave: in its group; t: a group's k-tile, which is the block's k-tile GK * t + group)
-        __device__ __forceinline__ Source(const I8Args &g, const I8Tile &tile, uint32_t wave, uint32_t lane) : cols(g, tile) {
+        __device__ __forceinline__ Source(const I8Args &g, const I8Tile &tile, const CopyRows &rows, uint32_t wave, uint32_t lane) : cols(g, tile) {
             a = GROUPED ? i8_rsrc(g.A, g.a_rows * g.lda) : i8_rsrc(g.A + (uint64_t)tile.row0 * g.lda, tile.rows * g.lda);
 #pragma unroll
             for (int i = 0; i < LA; ++i) {
                 const uint32_t row = wave * (LA * 8) + i * 8 + lane / 8u, kc = (lane & 7u) ^ i8_swizzle(row);
-                if constexpr (GROUPED) {
-                    const uint32_t s = row < tile.rows ? i8_source<true>(g, tile.row0 + row) : ~0u;
-                    off_a[i] = s == ~0u ? kOutside : s * g.lda + kc * 16u;
-                } else off_a[i] = row * g.lda + kc * 16u;
+                if constexpr (GROUPED) off_a[i] = rows.of_a[i] == ~0u ? kOutside : rows.of_a[i] * g.lda + kc * 16u;
+                else off_a[i] = row * g.lda + kc * 16u;
             }
 #pragma unroll
             for (int i = 0; i < LB; ++i) {
@@ -137,23 +148,33 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
     static constexpr int PER = GATED ? 2 : 1, NP = BN / PER;         // blocks of columns of C that a wave has
     // Where a wave's results lie -- lane l holds row l % 16, columns 4 * (l / 16) .. + 3 of every 16 x 16 block -- and what they are scaled with
     struct Finals {
-        uint32_t r0, c0, source[KEEP];
-        float sr[KEEP];
+        // (the four lanes of a row share out its blocks' rows of A, and pass the scales on)
+        static constexpr int MINE = (KEEP + 3) / 4;
+        uint32_t r0, c0, source[MINE];
+        float sr[MINE];
         I8Scales<GATED> scales[NP];
+        // the rows of A (by expert a read that scales wait for: asked for before the products), then all else
+        __device__ __forceinline__ void sources(const I8Args &g, const I8Tile &tile, uint32_t wave, uint32_t group, uint32_t lane) {
+#pragma unroll
+            for (int p = 0; p < MINE; ++p) {
+                const uint32_t i = (lane >> 4) * MINE + p, r = (wave / GN) * WM + (group * KEEP + i) * 16 + (lane & 15u);
+                source[p] = i < (uint32_t)KEEP && r < tile.rows ? i8_source<GROUPED>(g, tile.row0 + r) : ~0u;
+            }
+        }
         __device__ __forceinline__ void ask(const I8Args &g, const I8Tile &tile, const I8Columns<TN, GATED> &cols, uint32_t wave, uint32_t group, uint32_t lane) {
             r0 = (wave / GN) * WM + group * (KEEP * 16) + (lane & 15u);
             c0 = cols.first + (wave % GN) * (WN / PER) + (lane >> 4) * 4u;
-#pragma unroll
-            for (int i = 0; i < KEEP; ++i) source[i] = r0 + i * 16u < tile.rows ? i8_source<GROUPED>(g, tile.row0 + r0 + i * 16u) : ~0u;
 #pragma unroll
             for (int j = 0; j < NP; ++j) {
                 const uint32_t col = c0 + j * 16u;
                 scales[j].load(cols, g, tile, col < cols.of_c ? col : cols.of_c - 1u);
             }
-        }
-        __device__ __forceinline__ void rows(const I8Args &g) {
 #pragma unroll
-            for (int i = 0; i < KEEP; ++i) sr[i] = source[i] == ~0u ? 0.f : g.scale_a[source[i]];
+            for (int p = 0; p < MINE; ++p) sr[p] = source[p] == ~0u ? 0.f : g.scale_a[source[p]];
+        }
+        __device__ __forceinline__ void rows(uint32_t lane, float (&all)[KEEP]) const {
+#pragma unroll
+            for (int i = 0; i < KEEP; ++i) all[i] = __shfl(sr[i % MINE], (int)(i / MINE * 16 + (lane & 15u)));
         }
     };
     // Small waves ask for their scales before the products (128 x 4096 x 4096 9.9 -> 9.55 us, 1024 x 2304 x 768 8.35 -> 8.1); large ones have no
@@ -168,42 +189,54 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
         const uint32_t nk = ((g.k + 127u) / 128u + GK - 1u) / GK;    // k-tiles of a group (the last of the second may be nothing: it is cut)
         I8Tile tile = tiles.take(g, 0);
         if (!tile.some) return;
-        Source src(g, tile, wave, lane);
+        CopyRows rows;
+        rows.ask(g, tile, wave, lane);
+        Source src(g, tile, rows, wave, lane);
         Finals fin;
-        if constexpr (EARLY) fin.ask(g, tile, src.cols, wave, group, lane);
+        if constexpr (EARLY) {
+            fin.sources(g, tile, wave, group, lane);
+            fin.ask(g, tile, src.cols, wave, group, lane);
+        }
         fill(src, ring, wave, group, nk);
-        if constexpr (EARLY) fin.rows(g);
         for (uint32_t turn = 1;; ++turn) {
             i8_i32x4 acc[BM][BN];
 #pragma unroll
             for (int i = 0; i < BM; ++i)
 #pragma unroll
                 for (int j = 0; j < BN; ++j) acc[i][j] = i8_i32x4{0, 0, 0, 0};
-            auto take = [&] { return tiles.take(g, turn); };
+            const I8Tile next = tiles.take(g, turn);
+            if constexpr (GROUPED) {
+                fin.sources(g, tile, wave, group, lane);
+                if (next.some) rows.ask(g, next, wave, lane);
+            }
             // a wave whose part of the tile lies beyond the last row or column copies for the others, and leaves them the matrix cores
             const bool idle = (wave / GN) * WM >= tile.rows || src.cols.first + (wave % GN) * (WN / PER) >= src.cols.of_c;
-            const I8Tile next = idle ? copies_alone(src, ring, wave, group, nk, take) : products(g, src, ring, wave, group, lane, nk, acc, take);
+            if (idle) copies_alone(src, ring, wave, group, nk, turn > 1 && counted(g));
+            else products(g, src, ring, wave, group, lane, nk, turn > 1 && counted(g), acc);
             const I8Tile done = tile;
             const I8Columns<TN, GATED> cols = src.cols;
             i8_i32x4 kept[KEEP][BN];
             if constexpr (GK > 1) meet(smem, wave, group, lane, acc, kept);
+            uint32_t l = lane;
+            asm volatile("" : "+v"(l));                              // (nothing of what follows is worked out before the products and kept over them)
             if constexpr (!EARLY) {
-                fin.ask(g, done, cols, wave, group, lane);
-                fin.rows(g);
+                if constexpr (!GROUPED) fin.sources(g, done, wave, group, l);
+                fin.ask(g, done, cols, wave, group, l);
             }
             if (next.some) {
                 // (every wave has read the last k-tile: they met after its second k-step had arrived)
                 if constexpr (GK > 1) __syncthreads();               // the sums have been read
-                src = Source(g, next, wave, lane);
+                src = Source(g, next, rows, wave, l);
                 fill(src, ring, wave, group, nk);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            if constexpr (GK > 1) results(g, done, cols, fin, lane, kept);
-            else results(g, done, cols, fin, lane, acc);
+            if constexpr (GK > 1) results(g, done, cols, fin, l, kept);
+            else results(g, done, cols, fin, l, acc);
             if (!next.some) return;
             tile = next;
             if constexpr (EARLY) {
+                fin.sources(g, tile, wave, group, lane);
                 fin.ask(g, tile, src.cols, wave, group, lane);
-                fin.rows(g);
             }
         }
     }
@@ -228,11 +261,15 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
     }
 
     // k-tile 0 has landed / tile t has been read by this wave and tile t + 1 has landed.  In flight beyond it: A of t + 2 (slots), or the stages up
-    // to t + STAGES - 1.  (The last results' stores may be behind the first copies: the count then waits for some of them.)
-    static __device__ __forceinline__ void first_landed(uint32_t nk) {
-        constexpr int BEHIND = SLOTS ? 2 * LA + LB : (STAGES - 1) * (LA + LB);
-        if (nk >= (uint32_t)FAR) i8_wait_copies<BEHIND>();
-        else i8_wait_copies<0>();
+    // to t + STAGES - 1.  The last tile's results were stored after the first copies: where it is known how many stores those were (STORES at
+    // least), they may still be under way when the copies have landed.
+    static constexpr int STORES = KEEP * NP / (NP % 2 == 0 ? 2 : 1);
+    static __device__ __forceinline__ void first_landed(uint32_t nk, bool stores) {
+        constexpr int BEHIND = SLOTS ? 2 * LA + LB : (STAGES - 1) * (LA + LB), MOST = BEHIND + STORES < 63 ? BEHIND + STORES : 63;
+        if (nk >= (uint32_t)FAR) {
+            if (stores) i8_wait_copies<MOST>();
+            else i8_wait_copies<BEHIND>();
+        } else i8_wait_copies<0>();
         __builtin_amdgcn_s_barrier();
     }
     template <bool STEADY> static __device__ __forceinline__ void next_landed(uint32_t t, uint32_t nk) {
@@ -252,33 +289,29 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
         }
     }
 
-    template <typename NEXT>
-    __device__ static __forceinline__ I8Tile copies_alone(const Source &src, unsigned char *ring, uint32_t wave, uint32_t group, uint32_t nk, NEXT next) {
+    __device__ static __forceinline__ void copies_alone(const Source &src, unsigned char *ring, uint32_t wave, uint32_t group, uint32_t nk, bool stores) {
         uint32_t sa = 0, sb = A_BYTES, t = 0;
-        first_landed(nk);
+        first_landed(nk, stores);
         for (; t + FAR < nk; ++t) {
             next_landed<true>(t, nk);
             i8_each<0, LA + LB>([&](auto q) { copy_behind<decltype(q)::value, true>(src, ring, wave, group, t, nk, sa, sb); });
             sa = next_slot(sa); sb = next_slot(sb);
         }
-        const I8Tile after = next();
         for (; t < nk; ++t) {
             next_landed<false>(t, nk);
             i8_each<0, LA + LB>([&](auto q) { copy_behind<decltype(q)::value, false>(src, ring, wave, group, t, nk, sa, sb); });
             sa = next_slot(sa); sb = next_slot(sb);
         }
-        return after;
     }
 
-    template <typename NEXT>
-    __device__ static __forceinline__ I8Tile products(const I8Args &g, const Source &src, unsigned char *ring, uint32_t wave, uint32_t group, uint32_t lane, uint32_t nk, i8_i32x4 (&acc)[BM][BN], NEXT next) {
+    __device__ static __forceinline__ void products(const I8Args &g, const Source &src, unsigned char *ring, uint32_t wave, uint32_t group, uint32_t lane, uint32_t nk, bool stores, i8_i32x4 (&acc)[BM][BN]) {
         const uint32_t wm = wave / GN, wn = wave % GN;
         const uint32_t sbase = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)ring;
         const uint32_t ra = wm * WM + (lane & 15u), rb = wn * WN + (lane & 15u);
         const uint32_t fa = sbase + ra * 128u + (((lane >> 4) ^ i8_swizzle(ra)) << 4);
         const uint32_t fb = sbase + rb * 128u + (((lane >> 4) ^ i8_swizzle(rb)) << 4);
         uint32_t sa = 0, sb = A_BYTES;                               // slots of the tile being consumed
-        first_landed(nk);
+        first_landed(nk, stores);
         Frag f0, f1;
         read_range<0, 0, NR>(fa + sa, fb + sb, f0);
         auto step = [&](uint32_t t, auto steady_c) {
@@ -287,8 +320,10 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
             if constexpr (!STEADY) {
                 const uint32_t k0 = (t * GK + group) * 128u;
                 if (k0 + 128u > g.k) {
+                    uint32_t l = lane;
+                    asm volatile("" : "+v"(l));                      // (what the cut takes is worked out here, not kept over the loop)
 #pragma unroll
-                    for (int i = 0; i < BM; ++i) f0.a[i] = i8_cut(f0.a[i], k0 + (lane >> 4) * 16u, g.k);
+                    for (int i = 0; i < BM; ++i) f0.a[i] = i8_cut(f0.a[i], k0 + (l >> 4) * 16u, g.k);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -297,8 +332,10 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
             if constexpr (!STEADY) {
                 const uint32_t k0 = (t * GK + group) * 128u;
                 if (k0 + 128u > g.k) {
+                    uint32_t l = lane;
+                    asm volatile("" : "+v"(l));
 #pragma unroll
-                    for (int i = 0; i < BM; ++i) f1.a[i] = i8_cut(f1.a[i], k0 + 64u + (lane >> 4) * 16u, g.k);
+                    for (int i = 0; i < BM; ++i) f1.a[i] = i8_cut(f1.a[i], k0 + 64u + (l >> 4) * 16u, g.k);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -311,43 +348,85 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
         };
         uint32_t t = 0;
         for (; t + FAR < nk; ++t) step(t, std::true_type{});
-        const I8Tile after = next();
         for (; t < nk; ++t) step(t, std::false_type{});
         arrived(f0);                                                  // nothing of the last reads outlives the loop
-        return after;
     }
 
+    // Whether results are written with buffer stores, the same number by every wave
+    static __device__ __forceinline__ bool counted(const I8Args &g) { return g.out_kind ? g.vec : g.vec && g.through; }
     // Sums to C
     __device__ static __forceinline__ void results(const I8Args &g, const I8Tile &tile, const I8Columns<TN, GATED> &cols, const Finals &fin, uint32_t lane, const i8_i32x4 (&acc)[KEEP][BN]) {
         const uint32_t r0 = fin.r0, c0 = fin.c0, q4 = lane >> 4;
+        float sr[KEEP];
+        fin.rows(lane, sr);
         auto value = [&](int i, int j) -> i8_f32x4 {
-            if constexpr (GATED) return i8_gated(fin.scales[j], fin.sr[i], acc[i][2 * j], acc[i][2 * j + 1]);
-            else return i8_scaled(fin.scales[j], fin.sr[i], acc[i][j]);
+            if constexpr (GATED) return i8_gated(fin.scales[j], sr[i], acc[i][2 * j], acc[i][2 * j + 1]);
+            else return i8_scaled(fin.scales[j], sr[i], acc[i][j]);
         };
-        bool pairs = false;
-        if constexpr (NP % 2 == 0) pairs = g.vec && g.out_kind != 0;
-        if (pairs) {
-            // two neighbouring blocks: after the swap of odd and even 16-lane rows a lane holds 8 columns of one of them
-            uint16_t *const C = static_cast<uint16_t *>(g.C);
-            const uint32_t cc = c0 - q4 * 4u + (q4 & 1u) * 16u + (q4 >> 1) * 8u;
-#pragma unroll
-            for (int i = 0; i < KEEP; ++i)
-#pragma unroll
-                for (int j = 0; j + 1 < NP; j += 2) {
-                    const i8_f32x4 x = value(i, j), y = value(i, j + 1);
-                    const auto lo = __builtin_amdgcn_permlane16_swap(i8_pack(g.out_kind, x[0], x[1]), i8_pack(g.out_kind, y[0], y[1]), false, false);
-                    const auto hi = __builtin_amdgcn_permlane16_swap(i8_pack(g.out_kind, x[2], x[3]), i8_pack(g.out_kind, y[2], y[3]), false, false);
-                    const i8_u32x4 v = {lo[0], hi[0], lo[1], hi[1]};
-                    const uint32_t r = r0 + i * 16u, c = cc + j * 16u;
-                    if (r < tile.rows && c < cols.of_c) *reinterpret_cast<i8_u32x4 *>(C + (uint64_t)(tile.row0 + r) * g.ldc + c) = v;
-                }
-        } else {
+        if (!counted(g)) {
+            asm volatile("; results, single values");
 #pragma unroll
             for (int i = 0; i < KEEP; ++i)
 #pragma unroll
                 for (int j = 0; j < NP; ++j) {
                     const uint32_t r = r0 + i * 16u, col = c0 + j * 16u;
                     if (r < tile.rows && col < cols.of_c) i8_store4(g, tile.row0 + r, col, cols.of_c, value(i, j));
+                }
+            return;
+        }
+        // Buffer stores: what lies beyond the last row or column is dropped, so that every wave issues the same number of them (see first_landed)
+        const uint32_t es = g.out_kind ? 2u : 4u, pitch = g.ldc * es;
+        const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(static_cast<unsigned char *>(g.C) + (uint64_t)tile.row0 * pitch, 0, (int)((tile.rows - 1u) * pitch + cols.of_c * es), 0x00020000);
+        // (the row goes into the lane's offset, not into a scalar one: a 16-byte store with that may read its last register too late)
+        auto place = [&](uint32_t col) { return col < cols.of_c ? r0 * pitch + col * es : kOutside; };
+        if (g.out_kind == 0) {
+            asm volatile("; results, 32 bits");
+            uint32_t at[NP];
+#pragma unroll
+            for (int j = 0; j < NP; ++j) at[j] = place(c0 + j * 16u);
+#pragma unroll
+            for (int i = 0; i < KEEP; ++i) {
+#pragma unroll
+                for (int j = 0; j < NP; ++j) {
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i8_u32x4, value(i, j)), rc, (int)(at[j] + i * 16u * pitch), 0, 18);
+                    __builtin_amdgcn_sched_barrier(0);            // (left alone, the compiler scales everything first and spills)
+                }
+            }
+        } else if constexpr (NP % 2 == 0) {
+            // two neighbouring blocks: after the swap of odd and even 16-lane rows a lane holds 8 columns of one of them
+            const uint32_t cc = c0 - q4 * 4u + (q4 & 1u) * 16u + (q4 >> 1) * 8u;
+            auto store = [&](auto kind, auto policy) {
+                constexpr uint32_t KIND = decltype(kind)::value;
+                asm volatile("; results, kind %0, policy %1" ::"n"(KIND), "n"(decltype(policy)::value));
+                uint32_t at[NP / 2];
+#pragma unroll
+                for (int j = 0; j < NP; j += 2) at[j / 2] = place(cc + j * 16u);
+#pragma unroll
+                for (int i = 0; i < KEEP; ++i) {
+#pragma unroll
+                    for (int j = 0; j < NP; j += 2) {
+                        const i8_f32x4 x = value(i, j), y = value(i, j + 1);
+                        const auto lo = __builtin_amdgcn_permlane16_swap(i8_pack(KIND, x[0], x[1]), i8_pack(KIND, y[0], y[1]), false, false);
+                        const auto hi = __builtin_amdgcn_permlane16_swap(i8_pack(KIND, x[2], x[3]), i8_pack(KIND, y[2], y[3]), false, false);
+                        __builtin_amdgcn_raw_buffer_store_b128(i8_u32x4{lo[0], hi[0], lo[1], hi[1]}, rc, (int)(at[j / 2] + i * 16u * pitch), 0, decltype(policy)::value);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+            };
+            if (g.out_kind == 1u) {
+                if (g.through) store(std::integral_constant<uint32_t, 1>{}, std::integral_constant<int, 18>{});
+                else store(std::integral_constant<uint32_t, 1>{}, std::integral_constant<int, 0>{});
+            } else {
+                if (g.through) store(std::integral_constant<uint32_t, 2>{}, std::integral_constant<int, 18>{});
+                else store(std::integral_constant<uint32_t, 2>{}, std::integral_constant<int, 0>{});
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < KEEP; ++i)
+#pragma unroll
+                for (int j = 0; j < NP; ++j) {
+                    const i8_f32x4 x = value(i, j);
+                    __builtin_amdgcn_raw_buffer_store_b64(i8_u32x2{i8_pack(g.out_kind, x[0], x[1]), i8_pack(g.out_kind, x[2], x[3])}, rc, (int)(place(c0 + j * 16u) + i * 16u * pitch), 0, 0);
                 }
         }
     }

@@ -50,6 +50,7 @@ struct I8Args {
     uint32_t gated;                      // C has n / 2 columns, silu(gate) * value
     uint32_t out_kind;                   // 0 fp32, 1 fp16, 2 bf16
     uint32_t vec;                        // rows of C can be written 16 bytes (8 where C has 16 bits) at a time
+    uint32_t through;                    // rows of C lie on 64-byte blocks, and there are many: they are streamed and written through the L2
     uint32_t row_tiles, col_tiles;       // grid of the body that was chosen (grouped: the most row tiles there can be)
     uint32_t group;
     uint32_t cus;                        // compute units of the device
@@ -81,7 +82,11 @@ inline ft_status i8_check(const ft_i8_desc *d, bool grouped, uint32_t m, const i
     a->A = A; a->B = B; a->scale_a = scale_a; a->scale_b = scale_b; a->bias = bias; a->C = C;
     a->offsets = offsets; a->a_row = a_row;
     a->experts = d->experts; a->a_rows = a_rows;
-    a->vec = aligned_to(C, 16) && (uint64_t)a->ldc * es % 16u == 0 && columns % (16u / es) == 0;
+    // (256 rows within a buffer's 2 GB)
+    a->vec = aligned_to(C, 16) && (uint64_t)a->ldc * es % 16u == 0 && columns % (16u / es) == 0 && (uint64_t)a->ldc * es <= (4u << 20);
+    // Streamed and written through the L2 (64 x 128 tiles: 1024 x 2304 x 768 bf16, 4.7 MB, 8.1 us kept, 7.5 streamed; 4096 x 11008 x 768 58.8 and 50.9) or, where
+    // little is written, kept: the launch then ends a memory's latency earlier (128 x 4096 x 4096, 1 MB, 9.45 us kept, 9.7 streamed).
+    a->through = aligned_to(C, 64) && (uint64_t)a->ldc * es % 64u == 0 && (uint64_t)m * columns * es >= (4u << 20);
     *launch = true;
     return FT_OK;
 }

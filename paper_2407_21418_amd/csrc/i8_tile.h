@@ -53,32 +53,35 @@ __device__ __forceinline__ bool i8_position(uint32_t b, uint32_t grid, uint32_t 
     return j < q + (x < r ? 1u : 0u);
 }
 
-// The tiles of a launch.  By expert the counts of each are on the device: the lanes of a wave hold the experts' rows and prefix sums of
-// their row tiles (64 experts at a time).
+// The tiles of a launch.  By expert the counts of each are on the device: the lanes of a wave count 64 experts' row tiles at a time, and their
+// prefix sums, the first 64 of which stay for as long as the workgroup lives, say whose a tile is.
 template <int TM, int TN, bool GROUPED> struct I8Tiles {
-    uint32_t total;
+    uint32_t total, upto;                                    // all tiles; row tiles up to and with those of expert `lane`
     __device__ __forceinline__ I8Tiles(const I8Args &a) {
         if constexpr (!GROUPED) total = a.row_tiles * a.col_tiles;
         else {
-            uint32_t sum = 0, beg;
-            for (uint32_t at = 0; at < a.experts; at += 64u) sum += __builtin_amdgcn_readlane(scan((rows_of(a, at + (threadIdx.x & 63u), &beg) + TM - 1u) / TM), 63);
+            upto = upto_of(a, 0);
+            uint32_t sum = __builtin_amdgcn_readlane(upto, 63);
+            for (uint32_t at = 64; at < a.experts; at += 64u) sum += __builtin_amdgcn_readlane(upto_of(a, at), 63);
             total = sum * a.col_tiles;
         }
     }
-    // rows of expert e, from offsets that are held to 0 .. m
-    static __device__ __forceinline__ uint32_t rows_of(const I8Args &a, uint32_t e, uint32_t *beg) {
-        if (e >= a.experts) { *beg = 0; return 0u; }
-        int32_t s = a.offsets[e], n = a.offsets[e + 1];
+    struct Rows { uint32_t beg, count; };
+    // rows of expert e, from offsets that are held to 0 .. m (nothing writes them while the kernel runs: a uniform e reads them as constants)
+    static __device__ __forceinline__ Rows rows_of(const I8Args &a, uint32_t e) {
+        const auto *const o = (const __attribute__((address_space(4))) int32_t *)a.offsets;
+        int32_t s = o[e], n = o[e + 1];
         s = s < 0 ? 0 : s > (int32_t)a.m ? (int32_t)a.m : s;
         n = n < s ? s : n > (int32_t)a.m ? (int32_t)a.m : n;
-        *beg = (uint32_t)s;
-        return (uint32_t)(n - s);
+        return Rows{(uint32_t)s, (uint32_t)(n - s)};
     }
-    static __device__ __forceinline__ uint32_t scan(uint32_t v) {
+    static __device__ __forceinline__ uint32_t upto_of(const I8Args &a, uint32_t at) {
+        const uint32_t lane = threadIdx.x & 63u;
+        uint32_t v = at + lane < a.experts ? (rows_of(a, at + lane).count + TM - 1u) / TM : 0u;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
             const uint32_t up = __shfl_up(v, d);
-            if ((threadIdx.x & 63u) >= (uint32_t)d) v += up;
+            if (lane >= (uint32_t)d) v += up;
         }
         return v;
     }
@@ -100,21 +103,20 @@ template <int TM, int TN, bool GROUPED> struct I8Tiles {
         }
         uint32_t before = 0;
         for (uint32_t at = 0; at < a.experts; at += 64u) {
-            uint32_t beg;
-            const uint32_t count = rows_of(a, at + (threadIdx.x & 63u), &beg), tiles = (count + TM - 1u) / TM, upto = scan(tiles);
-            const uint64_t behind = __ballot((before + upto) * a.col_tiles > u);
+            const uint32_t here = at ? upto_of(a, at) : upto;
+            const uint64_t behind = __ballot((before + here) * a.col_tiles > u);
             if (behind) {
-                const int l = __builtin_ctzll(behind);
-                const uint32_t n_tiles = __builtin_amdgcn_readlane(tiles, l), w = u - (before + __builtin_amdgcn_readlane(upto, l) - n_tiles) * a.col_tiles;
-                const uint32_t col = w / n_tiles, row = w - col * n_tiles, rows = __builtin_amdgcn_readlane(count, l) - row * TM;
-                t.expert = at + (uint32_t)l;
-                t.row0 = __builtin_amdgcn_readlane(beg, l) + row * TM;
+                const uint32_t l = (uint32_t)__builtin_ctzll(behind), under = before + (l ? __builtin_amdgcn_readlane(here, l - 1u) : 0u);
+                const Rows r = rows_of(a, at + l);
+                const uint32_t n_tiles = (r.count + TM - 1u) / TM, w = u - under * a.col_tiles, col = w / n_tiles, row = w - col * n_tiles, rows = r.count - row * TM;
+                t.expert = at + l;
+                t.row0 = r.beg + row * TM;
                 t.rows = rows < (uint32_t)TM ? rows : (uint32_t)TM;
                 t.n0 = col * TN;
                 t.some = col < a.col_tiles;                  // (offsets that are not ascending can say otherwise)
                 return t;
             }
-            before += __builtin_amdgcn_readlane(upto, 63);
+            before += __builtin_amdgcn_readlane(here, 63);
         }
         t.some = false;                                      // (not reached: u < total)
         return t;
