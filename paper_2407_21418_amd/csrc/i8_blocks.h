@@ -15,19 +15,19 @@ struct I8KindInfo {
     // few its tiles are; the second is what they share: the caches' bandwidth and the power.
     float once, round, round_k, tile, tile_k;
 };
-// Least squares over 204 shapes, m 8 .. 4096, n 768 .. 11008, k 768 .. 4096, all kinds measured at each (bf16 results, an idle device): the times
-// are met to 3 .. 9 % (root of the mean square), and the kind with the least is within 0.5 % of the fastest on average, 6 % at most.
+// Least squares over 216 shapes, m 8 .. 8192, n 768 .. 11008, k 768 .. 4096, all kinds measured at each (bf16 results, an idle device): the times
+// are met to 4 .. 15 % (root of the mean square), and the kind with the least is within 0.2 % of the fastest on average, 8 % at most.
 constexpr I8KindInfo kI8Kinds[I8_KINDS] = {
-    {16, 16, 1, 2.85f, 0.43f, 0.096f, 0.17f, 0.012f},
-    {64, 64, 1, 2.88f, 0.92f, 0.153f, 1.02f, 0.028f},
-    {64, 128, 2, 3.69f, 0.46f, 0.240f, 1.93f, 0.249f},
-    {128, 128, 2, 3.99f, 0.00f, 0.459f, 3.61f, 0.388f},
-    {128, 256, 1, 3.59f, 2.10f, 0.539f, 2.85f, 0.159f},
-    {256, 256, 1, 3.96f, 3.85f, 0.949f, 5.16f, 0.193f},
+    {16, 16, 1, 2.79f, 0.29f, 0.080f, 0.12f, 0.018f},
+    {64, 64, 1, 2.95f, 1.12f, 0.142f, 0.76f, 0.045f},
+    {64, 128, 2, 3.08f, 1.02f, 0.228f, 0.85f, 0.300f},
+    {128, 128, 2, 3.59f, 0.00f, 0.442f, 3.11f, 0.431f},
+    {128, 256, 1, 2.82f, 2.67f, 0.440f, 1.91f, 0.346f},
+    {256, 256, 1, 2.37f, 4.99f, 0.694f, 3.79f, 0.701f},
 };
 inline I8KindInfo i8_kind_info(I8Kind kind, bool gated) {
     I8KindInfo i = kI8Kinds[kind];
-    if (kind == I8_STREAM && gated) i.tn = 32;
+    if (kind == I8_STREAM && gated) i.tn = 32, i.tile *= 2.f, i.tile_k *= 2.f;      // twice the columns
     return i;
 }
 
@@ -42,7 +42,11 @@ inline float i8_time(const I8Args &a, I8Kind kind, bool grouped) {
     const float tiles = i8_row_tiles(a, i.tm, grouped) * (float)((a.n + i.tn - 1u) / i.tn), share = tiles / (float)(a.cus * i.per_cu), k = (float)((a.k + 127u) / 128u);
     float rounds = (float)(uint32_t)share;
     if (rounds < share) rounds += 1.f;
-    return i.once + rounds * (i.round + i.round_k * k) + share * (i.tile + i.tile_k * k);
+    // By expert a tile first reads where its rows lie, then their numbers: a microsecond more.  Blocks ask for the next tile's ahead; the first kind
+    // waits anew once for what a CU holds, four workgroups, two with gates (4 tokens, 2 of 16 experts, 2816 x 2048 gated: 12.2 us in three
+    // rounds of the first kind, 10.7 in one of the third, which are both expected at 9.7 without this).
+    const float held = kind == I8_STREAM ? (a.gated ? 2.f : 4.f) : rounds, waits = grouped ? (float)(uint32_t)((rounds + held - 1.f) / held) : 0.f;
+    return i.once + waits + rounds * (i.round + i.round_k * k) + share * (i.tile + i.tile_k * k);
 }
 inline I8Kind i8_choose(const I8Args &a, bool grouped) {
     I8Kind best = I8_STREAM;
