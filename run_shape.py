@@ -3,6 +3,7 @@
     python run_shape.py --m 8192 --n 4096 --k 4096 --dtype bf16 --iters 20
     ... --force 256,256,128,128     # force the single-uKernel program (tm,tn,wm,wn), M % tm == 0
     ... --baseline                  # the pad-to-library plan
+    ... --dtype i8                  # rows quantised to 8-bit integers (ft_i8_quantize) and their product (ft_i8_matmul), bf16 in and out
 
 Prints one line: shape, program, tiles, microseconds per launch, TFLOP/s, GB/s (algorithmic bytes).
 """
@@ -19,12 +20,54 @@ def form_name(ft, form):
     return names.get(form, "form %d" % form)
 
 
+def run_i8(a):
+    """A linear layer in 8-bit integers: the rows' quantisation and the product, each timed alone and both in turn."""
+    import torch
+    import paper_2407_21418_amd as ft
+
+    m, n, k, pitch = a.m, a.n, a.k, (a.k + 15) // 16 * 16        # rows of 8-bit operands lie on 16-byte blocks
+    out, xs = 2 * m * n, 2 * m * k
+    bytes_alg = m * k + n * k + 4 * (m + n) + out
+    nsets = max(1, int(a.ring_mb * 1e6 // bytes_alg))
+    X = [torch.randn(m, k, device="cuda").to(torch.bfloat16) for _ in range(nsets)]
+    B = [torch.randint(-127, 128, (n, pitch), device="cuda", dtype=torch.int8) for _ in range(nsets)]
+    A = [torch.empty(m, pitch, device="cuda", dtype=torch.int8) for _ in range(nsets)]
+    C = [torch.empty(m, n, device="cuda", dtype=torch.bfloat16) for _ in range(nsets)]
+    sa, sb = torch.empty(m, device="cuda"), torch.rand(n, device="cuda")
+    quant, prod = ft.ft_quant_desc(cols=k, dtype=ft.FT_BF16), ft.ft_i8_desc(n=n, k=k, dtype=ft.FT_BF16, out_dtype=ft.FT_OUT_SAME)
+    s = torch.cuda.current_stream().cuda_stream
+
+    def quantize(i):
+        ft.ft_i8_quantize(quant, m, X[i].data_ptr(), A[i].data_ptr(), sa.data_ptr(), s)
+
+    def product(i):
+        ft.ft_i8_matmul(prod, m, A[i].data_ptr(), sa.data_ptr(), B[i].data_ptr(), sb.data_ptr(), 0, C[i].data_ptr(), s)
+
+    def both(i):
+        quantize(i)
+        product(i)
+
+    def timed(f):
+        for i in range(max(1, a.warmup, nsets)):
+            f(i % nsets)
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        for i in range(a.iters):
+            f(i % nsets)
+        e1.record()
+        e1.synchronize()
+        return e0.elapsed_time(e1) * 1e3 / a.iters
+    us_both, us_quant, us_prod = timed(both), timed(quantize), timed(product)
+    print("%dx%dx%d i8: quantise %.2f us, %.0f GB/s; product %.2f us, %.1f TOP/s, %.0f GB/s; both %.2f us" % (
+        m, n, k, us_quant, (xs + m * k + 4 * m) / us_quant / 1e3, us_prod, 2.0 * m * n * k / us_prod / 1e6, bytes_alg / us_prod / 1e3, us_both), flush=True)
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--m", type=int, required=True)
     ap.add_argument("--n", type=int, required=True)
     ap.add_argument("--k", type=int, required=True)
-    ap.add_argument("--dtype", default="f16", choices=["f16", "bf16"])
+    ap.add_argument("--dtype", default="f16", choices=["f16", "bf16", "i8"])
     ap.add_argument("--iters", type=int, default=50)
     ap.add_argument("--warmup", type=int, default=5)
     ap.add_argument("--force", default="")
@@ -37,6 +80,10 @@ def main():
     ap.add_argument("--copy-mb", type=float, default=0.0,
                     help="also run a plain device copy of this many MB (calibrates FETCH_SIZE / WRITE_SIZE)")
     a = ap.parse_args()
+    if a.dtype == "i8":
+        if a.force or a.baseline or a.zeta or a.copy_mb:
+            ap.error("--dtype i8 has no plan: --force, --baseline, --zeta and --copy-mb do not go with it")
+        return run_i8(a)
 
     import torch
     import paper_2407_21418_amd as ft
