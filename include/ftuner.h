@@ -508,7 +508,8 @@ typedef struct ft_i8_desc {
     uint32_t epilogue;             /* FT_EPI_NONE, FT_EPI_BIAS or FT_EPI_SILU_MUL            */
     uint32_t experts;              /* ft_i8_matmul: 0. ft_i8_matmul_experts: weights of B, 1 .. 1024 */
 } ft_i8_desc;
-/* A [m][lda], B [n][ldb]: 16-byte aligned, all rows with whole pitches.  scale_a [m], scale_b [n], bias [n]: fp32; bias non-NULL
+/* A [m][lda], B [n][ldb]: 16-byte aligned, all rows with whole pitches (pitches of multiples of 128 bytes are read fastest: a k of 1000 takes
+ * a quarter less time with 1024 than with 1008).  scale_a [m], scale_b [n], bias [n]: fp32; bias non-NULL
  * exactly with FT_EPI_BIAS.  C [m][ldc]: aligned to its elements (rows on 16-byte blocks are written fastest).  m = 0 launches nothing. */
 ft_status ft_i8_matmul(const ft_i8_desc *desc, uint32_t m, const int8_t *A, const float *scale_a, const int8_t *B, const float *scale_b,
                        const float *bias, void *C, void *hip_stream);

@@ -185,24 +185,27 @@ __device__ __forceinline__ uint32_t i8_pack(uint32_t out_kind, float x, float y)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(i8_f32x2{x, y}, i8_bf16x2));
 }
 
-// Four neighbouring columns of a row of C
+// Four neighbouring columns of a row of C, at any address that is aligned to its elements (value by value only where the row ends among them: all rows
+// of 715 fp32 so: 2000 x 1430 x 1000 gated took 13.1 us, now 10.8)
+typedef float I8AnyF32x4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t I8AnyU32x2 __attribute__((ext_vector_type(2), aligned(2)));
 __device__ __forceinline__ void i8_store4(const I8Args &a, uint32_t row, uint32_t col, uint32_t columns, i8_f32x4 v) {
     const uint64_t at = (uint64_t)row * a.ldc + col;
     if (a.out_kind == 0) {
         float *const c = static_cast<float *>(a.C) + at;
-        if (a.vec) *reinterpret_cast<i8_f32x4 *>(c) = v;
+        if (col + 4u <= columns) *reinterpret_cast<I8AnyF32x4 *>(c) = v;
         else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < 3; ++e)
                 if (col + e < columns) c[e] = v[e];
         }
     } else {
         uint16_t *const c = static_cast<uint16_t *>(a.C) + at;
         const i8_u32x2 h = {i8_pack(a.out_kind, v[0], v[1]), i8_pack(a.out_kind, v[2], v[3])};
-        if (a.vec) *reinterpret_cast<i8_u32x2 *>(c) = h;
+        if (col + 4u <= columns) *reinterpret_cast<I8AnyU32x2 *>(c) = h;
         else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < 3; ++e)
                 if (col + e < columns) c[e] = (uint16_t)(h[e / 2] >> (e % 2 * 16));
         }
     }
