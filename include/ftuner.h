@@ -15,6 +15,8 @@
  *   (d) ft_launch           one launch over the tile-descriptor table       (Sec. 3: uKernel = thread block)
  *                           (ft_plan_launch_form: or over row runs, large blocks, image patches,
  *                           one grid of equal tiles)
+ * Beside them stand calls that need no plan: matmuls in 8-bit integers, whose kernel is chosen at
+ * the launch, and what sorts a batch's tokens by expert for them (e).
  *
  * Conventions
  *   - Plain C, no exceptions cross the boundary; every call returns ft_status (0 = FT_OK).
@@ -509,7 +511,7 @@ typedef struct ft_i8_desc {
     uint32_t experts;              /* ft_i8_matmul: 0. ft_i8_matmul_experts: weights of B, 1 .. 1024 */
 } ft_i8_desc;
 /* A [m][lda], B [n][ldb]: 16-byte aligned, all rows with whole pitches (pitches of multiples of 128 bytes are read fastest: a k of 1000 takes
- * a quarter less time with 1024 than with 1008).  scale_a [m], scale_b [n], bias [n]: fp32; bias non-NULL
+ * a fifth less time with 1024 than with 1008).  scale_a [m], scale_b [n], bias [n]: fp32; bias non-NULL
  * exactly with FT_EPI_BIAS.  C [m][ldc]: aligned to its elements (rows on 16-byte blocks are written fastest).  m = 0 launches nothing. */
 ft_status ft_i8_matmul(const ft_i8_desc *desc, uint32_t m, const int8_t *A, const float *scale_a, const int8_t *B, const float *scale_b,
                        const float *bias, void *C, void *hip_stream);

