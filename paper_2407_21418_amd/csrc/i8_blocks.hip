@@ -112,8 +112,11 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
         __amdgpu_buffer_rsrc_t a;
         I8Columns<TN, GATED> cols;
         uint32_t off_a[LA], off_b[LB];
+        uint32_t first_k, whole_k;
         // (wave: in its group; t: a group's k-tile, which is the block's k-tile GK * t + group)
         __device__ __forceinline__ Source(const I8Args &g, const I8Tile &tile, const CopyRows &rows, uint32_t wave, uint32_t lane) : cols(g, tile) {
+            whole_k = g.k / (128u * GK);
+            first_k = g.k >= 8192u ? (blockIdx.x & 7u) * whole_k / 8u : 0u;
             a = GROUPED ? i8_rsrc(g.A, g.a_rows * g.lda) : i8_rsrc(g.A + (uint64_t)tile.row0 * g.lda, tile.rows * g.lda);
 #pragma unroll
             for (int i = 0; i < LA; ++i) {
@@ -127,12 +130,23 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
                 off_b[i] = ((GATED ? row / 32u * 16u + (row & 15u) : row) * g.ldb) + kc * 16u;
             }
         }
+        // Where the t-th k-tile that is taken begins.  Through a long reduce axis every XCD goes from another place on, and round to there (a last k-tile that
+        // the axis ends inside stays the last one): they do not all ask for the same part of the same rows then.  128 x 256: 2048 x 4096 x 11008 89 us all
+        // from the beginning, 85.5 so, 2048 x 5120 x 13824 180 and 173, 2048 x 4096 x 4096 32 both; 256 x 256 has no scalar instructions to spare in
+        // its loop: 8192 x 8192 x 8192 396 and 404.
+        __device__ __forceinline__ uint32_t at_k(uint32_t t, uint32_t group) const {
+            if constexpr (!SLOTS) {
+                const uint32_t x = t + first_k;
+                t = t >= whole_k ? t : x >= whole_k ? x - whole_k : x;
+            }
+            return t * (128u * GK) + group * 128u;
+        }
         template <int I> __device__ __forceinline__ void copy_a(unsigned char *smem, uint32_t wave, uint32_t group, uint32_t t, uint32_t slot) const {
-            i8_copy(a, smem + slot + wave * (LA * 1024) + I * 1024, off_a[I], t * (128u * GK) + group * 128u);
+            i8_copy(a, smem + slot + wave * (LA * 1024) + I * 1024, off_a[I], at_k(t, group));
         }
         template <int I> __device__ __forceinline__ void copy_b(unsigned char *smem, uint32_t wave, uint32_t group, uint32_t t, uint32_t slot) const {
             const bool values = GATED && (((wave * (LB * 8) + I * 8) / 16u) & 1u);
-            i8_copy(values ? cols.values : cols.b, smem + slot + wave * (LB * 1024) + I * 1024, off_b[I], t * (128u * GK) + group * 128u);
+            i8_copy(values ? cols.values : cols.b, smem + slot + wave * (LB * 1024) + I * 1024, off_b[I], at_k(t, group));
         }
     };
     static __device__ __forceinline__ uint32_t next_slot(uint32_t s) {

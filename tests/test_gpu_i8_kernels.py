@@ -23,6 +23,18 @@ def spread(rows, experts):
 
 @pytest.mark.parametrize("name,m,n,k,gates,experts", CASES)
 def test_kernel(name, m, n, k, gates, experts):
+    check_product(m, n, k, gates, experts)
+
+
+# a reduce axis that every XCD goes through from another place on, ended inside a block, at its end and inside the last of two groups' blocks
+@pytest.mark.parametrize("m,n,k,gates,experts", [(300, 776, 8191, False, 0), (300, 776, 8192, False, 0), (700, 1040, 9000, False, 0), (1300, 1040, 8449, False, 0), (300, 4112, 8200, True, 0),
+                                                 (1030, 4112, 8320, False, 0), (770, 5136, 11008, True, 0), (2060, 4112, 9000, False, 0), (200, 1040, 8300, False, 7), (1000, 4112, 8192, True, 7),
+                                                 (2570, 2064, 8200, False, 7)])
+def test_long_reduce_axes(m, n, k, gates, experts):
+    check_product(m, n, k, gates, experts)
+
+
+def check_product(m, n, k, gates, experts):
     weights, of_c = max(1, experts), n // 2 if gates else n
     p = Problem(min(m, 3000) if experts else m, n, k, experts=weights, bias=not gates and m % 2 == 0)
     if gates:
