@@ -15,15 +15,15 @@ struct I8KindInfo {
     // few its tiles are; the second is what they share: the caches' bandwidth and the power.
     float once, round, round_k, tile, tile_k;
 };
-// Least squares over 216 shapes, m 8 .. 8192, n 768 .. 11008, k 768 .. 4096, all kinds measured at each (bf16 results, an idle device): the times
-// are met to 4 .. 15 % (root of the mean square), and the kind with the least is within 0.2 % of the fastest on average, 8 % at most.
+// Least squares over 348 shapes, m 8 .. 32768, n 768 .. 11008, k 64 .. 4096, all kinds measured at each (bf16 results, an idle device): the times
+// are met to 5 .. 13 % (root of the mean square), and the kind with the least is within 0.3 % of the fastest on average, 10 % at most.
 constexpr I8KindInfo kI8Kinds[I8_KINDS] = {
-    {16, 16, 1, 2.79f, 0.29f, 0.080f, 0.12f, 0.018f},
-    {64, 64, 1, 2.95f, 1.12f, 0.142f, 0.76f, 0.045f},
-    {64, 128, 2, 3.08f, 1.02f, 0.228f, 0.85f, 0.300f},
-    {128, 128, 2, 3.59f, 0.00f, 0.442f, 3.11f, 0.431f},
-    {128, 256, 1, 2.82f, 2.67f, 0.440f, 1.91f, 0.346f},
-    {256, 256, 1, 2.37f, 4.99f, 0.694f, 3.79f, 0.701f},
+    {16, 16, 1, 2.60f, 0.11f, 0.101f, 0.13f, 0.000f},
+    {64, 64, 1, 2.92f, 1.22f, 0.141f, 0.57f, 0.053f},
+    {64, 128, 2, 2.63f, 1.49f, 0.233f, 0.85f, 0.306f},
+    {128, 128, 2, 3.30f, 0.60f, 0.426f, 2.93f, 0.422f},
+    {128, 256, 1, 2.93f, 2.37f, 0.458f, 1.87f, 0.349f},
+    {256, 256, 1, 2.15f, 5.08f, 0.710f, 2.90f, 0.707f},
 };
 inline I8KindInfo i8_kind_info(I8Kind kind, bool gated) {
     I8KindInfo i = kI8Kinds[kind];
@@ -47,9 +47,9 @@ inline float i8_time(const I8Args &a, I8Kind kind, bool grouped) {
     // waits anew once for what a CU holds, four workgroups, two with gates (4 tokens, 2 of 16 experts, 2816 x 2048 gated: 11.8 us in three
     // rounds of the first kind, 10.5 in one of the third, which are both expected at 9.7 without this).
     const float held = kind == I8_STREAM ? (a.gated ? 2.f : 4.f) : rounds, waits = grouped ? (float)(uint32_t)((rounds + held - 1.f) / held) : 0.f;
-    // ... and each row of tiles reads its expert's weights, which other rows of tiles seldom find in the caches: 30 us a GB (32 products of 256 .. 65536
-    // entries and 8 .. 64 experts, all kinds measured: the chosen one is 1.7 % slower than the fastest on average, without this term 3.1 %).
-    const float weights = grouped ? 3e-8f * row_tiles * (float)a.n * (float)a.k : 0.f;
+    // ... and each row of tiles reads its expert's weights, which other rows of tiles seldom find in the caches: 10 us a GB (32 products of 256 .. 65536
+    // entries and 8 .. 64 experts, all kinds measured: the chosen one is 1.3 % slower than the fastest on average, without this term 3.1 %).
+    const float weights = grouped ? 1e-8f * row_tiles * (float)a.n * (float)a.k : 0.f;
     return i.once + waits + weights + rounds * (i.round + i.round_k * k) + share * (i.tile + i.tile_k * k);
 }
 inline I8Kind i8_choose(const I8Args &a, bool grouped) {

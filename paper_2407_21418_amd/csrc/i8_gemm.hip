@@ -24,8 +24,9 @@ namespace ftk {
 // Few rows: tiles of 16 rows by 16 columns (by 16 gates and their values) whose eight waves take turns along the reduce axis, 128 bytes of it
 // at a time, straight from memory into the matrix cores' operands, AHEAD turns under way; their sums meet in LDS.  Every byte of either
 // operand is loaded by one wave of a workgroup once.  What the sums are scaled with is asked for before the products.  Bound by one read of the
-// weight from the caches or memory, or by latency where that is small: 1 x 4096 x 4096 5.4 us (3.1 TB/s), 1 x 768 x 768 gated 3.8, 16 x 8192 x 2048
-// gated 6.1; 1 x 22016 x 4096 gated 22.7 (4.0 TB/s).
+// weight from the caches or memory, or by latency where that is small: 1 x 4096 x 4096 5.6 us (3.0 TB/s), 1 x 768 x 768 2.8, with gates 3.2, 16 x 8192
+// x 2048 gated 6.1; 1 x 22016 x 4096 gated 22.4 (4.0 TB/s).  A wave that has no turn left asks for nothing: loads whose results are zeros cost their
+// issue all the same (77 x 768 x 768, six turns for eight waves, 3.5 us with them, 3.1 without; 4 tokens, 2 of 8 experts, 1408 x 1024 gated 9.2 and 7.3).
 template <int AHEAD, bool GROUPED, bool GATED> __global__ __launch_bounds__(512) void ft_i8_stream(I8Args a) {
     constexpr int W = 8, NB = GATED ? 2 : 1;
     __shared__ i8_i32x4 sums[W][NB][64];
@@ -44,7 +45,8 @@ template <int AHEAD, bool GROUPED, bool GATED> __global__ __launch_bounds__(512)
             for (int j = 0; j < NB; ++j) f.b[h][j] = i8_load(cols.operand(j), s * 128u + h * 64u + kc < a.k ? off_b + s * 128u + h * 64u : kOutside);
     };
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) load_b(wave + i * W, f[i]);
+    for (int i = 0; i < AHEAD; ++i)
+        if (wave + i * W < steps) load_b(wave + i * W, f[i]);
     const __amdgpu_buffer_rsrc_t ar = GROUPED ? i8_rsrc(a.A, a.a_rows * a.lda) : i8_rsrc(a.A + (uint64_t)t.row0 * a.lda, t.rows * a.lda);
     const uint32_t off_a = GROUPED ? (source == ~0u ? kOutside : source * a.lda + kc) : r * a.lda + kc;
     auto load_a = [&](uint32_t s, Step &f) {
@@ -52,7 +54,8 @@ template <int AHEAD, bool GROUPED, bool GATED> __global__ __launch_bounds__(512)
         for (int h = 0; h < 2; ++h) f.a[h] = i8_load(ar, s * 128u + h * 64u + kc < a.k ? off_a + s * 128u + h * 64u : kOutside);
     };
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) load_a(wave + i * W, f[i]);
+    for (int i = 0; i < AHEAD; ++i)
+        if (wave + i * W < steps) load_a(wave + i * W, f[i]);
     // wave 0 has the tile's results: row r, four columns from `col`
     const uint32_t col = cols.first + (lane >> 4) * 4u;
     const bool mine = wave == 0 && r < t.rows && col < cols.of_c;
@@ -68,7 +71,8 @@ template <int AHEAD, bool GROUPED, bool GATED> __global__ __launch_bounds__(512)
     for (uint32_t s = wave; s < steps; s += AHEAD * W) {
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            const uint32_t now = s + i * W;                  // (beyond the last step: zeros)
+            const uint32_t now = s + i * W;
+            if (now >= steps) break;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 if (now * 128u + 128u > a.k) f[i].a[h] = i8_cut(f[i].a[h], now * 128u + h * 64u + kc, a.k);      // rows end inside the last step

@@ -55,7 +55,7 @@ __device__ __forceinline__ bool i8_position(uint32_t b, uint32_t grid, uint32_t 
 
 // The tiles of a launch.  By expert the counts of each are on the device: the lanes of a wave count 64 experts' row tiles at a time, and their
 // prefix sums, the first 64 of which stay for as long as the workgroup lives, say whose a tile is.  The first tile takes its rows from those lanes and
-// sums by lane moves, as nothing runs beside them then (4 tokens, 2 of 16 experts 10.8 -> 10.5 us, 300 of 8 5.8 -> 5.5).
+// sums by lane moves, as nothing runs beside them then (4 tokens, 2 of 16 experts 10.8 -> 10.5 us).
 template <int TM, int TN, bool GROUPED> struct I8Tiles {
     struct Rows { uint32_t beg, count; };
     uint32_t total, upto;                                    // all tiles; row tiles up to and with those of expert `lane`

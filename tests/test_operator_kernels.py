@@ -28,19 +28,20 @@ extern "C" int grid(unsigned m, unsigned n, int kind, int gated, int experts, un
 
 # kernel, m, n, k, gates, experts (0: a plain product): one tile for a workgroup at most, and several
 CASES = [
-    ("stream", 33, 80, 65, False, 0), ("stream", 33, 2064, 65, False, 0), ("64x64", 33, 2064, 2100, False, 0), ("64x128", 33, 8208, 65, False, 0), ("128x128", 130, 1040, 65, False, 0),
-    ("128x128", 1025, 8208, 65, False, 0), ("128x256", 770, 5136, 4100, False, 0), ("128x256", 4100, 4112, 4100, False, 0), ("256x256", 1025, 8208, 2100, False, 0),
-    ("256x256", 5130, 5136, 1100, False, 0), ("stream", 33, 80, 65, False, 7), ("stream", 130, 528, 65, False, 7), ("64x64", 33, 776, 4100, False, 7), ("64x128", 33, 2064, 65, False, 7),
-    ("64x128", 517, 8208, 65, False, 7), ("128x128", 517, 264, 65, False, 7), ("128x128", 1025, 8208, 65, False, 7), ("128x256", 300, 8208, 4100, False, 7), ("128x256", 2570, 5136, 2100, False, 7),
-    ("256x256", 4100, 2064, 1100, False, 7), ("256x256", 12300, 2064, 776, False, 7), ("stream", 33, 80, 65, False, 70), ("stream", 1025, 80, 65, False, 70), ("64x64", 33, 264, 776, False, 70),
-    ("64x128", 33, 528, 65, False, 70), ("64x128", 770, 5136, 65, False, 70), ("128x128", 4100, 80, 65, False, 70), ("128x128", 16390, 528, 65, False, 70), ("128x256", 5130, 2320, 4100, False, 70),
-    ("256x256", 12300, 528, 4100, False, 70), ("256x256", 16390, 2320, 4100, False, 70), ("stream", 33, 80, 65, True, 0), ("stream", 33, 2064, 65, True, 0), ("64x64", 33, 4112, 1100, True, 0),
-    ("64x128", 33, 8208, 65, True, 0), ("128x128", 130, 2064, 65, True, 0), ("128x128", 1025, 8208, 65, True, 0), ("128x256", 770, 5136, 4100, True, 0), ("128x256", 4100, 4112, 4100, True, 0),
-    ("256x256", 1025, 8208, 2100, True, 0), ("256x256", 5130, 5136, 1100, True, 0), ("stream", 33, 80, 65, True, 7), ("stream", 33, 2064, 65, True, 7), ("64x64", 33, 2064, 4100, True, 7),
-    ("64x128", 33, 4112, 65, True, 7), ("64x128", 517, 8208, 65, True, 7), ("128x128", 300, 776, 65, True, 7), ("128x128", 1025, 8208, 65, True, 7), ("128x256", 300, 8208, 4100, True, 7),
-    ("128x256", 2570, 5136, 2100, True, 7), ("256x256", 4100, 2064, 1100, True, 7), ("256x256", 12300, 2064, 776, True, 7), ("stream", 33, 80, 65, True, 70), ("stream", 1025, 80, 65, True, 70),
-    ("64x64", 33, 264, 4100, True, 70), ("64x128", 33, 528, 65, True, 70), ("64x128", 770, 5136, 65, True, 70), ("128x128", 4100, 80, 65, True, 70), ("128x128", 16390, 528, 65, True, 70),
-    ("128x256", 5130, 2320, 4100, True, 70), ("256x256", 12300, 528, 4100, True, 70), ("256x256", 16390, 2320, 4100, True, 70)]
+    ("stream", 33, 80, 65, False, 0), ("stream", 33, 2064, 65, False, 0), ("64x64", 33, 2064, 4100, False, 0), ("64x128", 1300, 264, 65, False, 0), ("128x128", 12300, 264, 65, False, 0),
+    ("128x128", 1300, 6160, 65, False, 0), ("128x256", 2570, 8208, 4100, False, 0), ("256x256", 1025, 8208, 1100, False, 0), ("256x256", 3300, 8208, 520, False, 0),
+    ("stream", 33, 80, 65, False, 7), ("stream", 33, 2064, 65, False, 7), ("64x64", 33, 776, 4100, False, 7), ("64x128", 33, 2320, 1100, False, 7), ("64x128", 1025, 6160, 65, False, 7),
+    ("128x128", 517, 6160, 65, False, 7), ("128x128", 1300, 6160, 65, False, 7), ("128x256", 517, 8208, 2100, False, 7), ("128x256", 1300, 8208, 4100, False, 7),
+    ("256x256", 2300, 3600, 1100, False, 7), ("256x256", 12300, 2064, 520, False, 7), ("stream", 33, 80, 65, False, 70), ("stream", 1025, 80, 65, False, 70),
+    ("64x64", 33, 264, 2100, False, 70), ("64x128", 33, 776, 65, False, 70), ("64x128", 770, 5136, 65, False, 70), ("128x128", 5130, 528, 65, False, 70),
+    ("128x128", 16390, 528, 65, False, 70), ("128x256", 5130, 2320, 6200, False, 70), ("stream", 33, 80, 65, True, 0), ("stream", 33, 2064, 65, True, 0), ("64x64", 1500, 80, 4100, True, 0),
+    ("64x128", 130, 4112, 65, True, 0), ("128x128", 12300, 264, 65, True, 0), ("128x128", 1300, 6160, 65, True, 0), ("128x256", 2570, 8208, 4100, True, 0),
+    ("256x256", 1025, 8208, 1100, True, 0), ("256x256", 3300, 8208, 520, True, 0), ("stream", 33, 80, 65, True, 7), ("stream", 33, 2064, 65, True, 7), ("64x64", 130, 776, 4100, True, 7),
+    ("64x128", 33, 3600, 65, True, 7), ("64x128", 1025, 6160, 65, True, 7), ("128x128", 517, 6160, 65, True, 7), ("128x128", 1300, 6160, 65, True, 7), ("128x256", 517, 8208, 2100, True, 7),
+    ("128x256", 1300, 8208, 4100, True, 7), ("256x256", 2300, 3600, 1100, True, 7), ("256x256", 12300, 2064, 520, True, 7), ("stream", 33, 80, 65, True, 70),
+    ("stream", 1025, 80, 65, True, 70), ("64x64", 2300, 80, 300, True, 70), ("64x128", 33, 528, 65, True, 70), ("64x128", 770, 5136, 65, True, 70), ("128x128", 5130, 528, 65, True, 70),
+    ("128x128", 16390, 528, 65, True, 70), ("128x256", 5130, 2320, 6200, True, 70),
+    ("256x256", 66000, 2832, 2048, False, 70), ("256x256", 66000, 2832, 2048, True, 70)]
 
 
 @pytest.fixture(scope="module")
