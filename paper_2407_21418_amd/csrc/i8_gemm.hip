@@ -26,7 +26,7 @@ namespace ftk {
 // operand is loaded by one wave of a workgroup once.  What the sums are scaled with is asked for before the products.  Bound by one read of the
 // weight from the caches or memory, or by latency where that is small: 1 x 4096 x 4096 5.6 us (3.0 TB/s), 1 x 768 x 768 2.8, with gates 3.2, 16 x 8192
 // x 2048 gated 6.1; 1 x 22016 x 4096 gated 22.4 (4.0 TB/s).  A wave that has no turn left asks for nothing: loads whose results are zeros cost their
-// issue all the same (77 x 768 x 768, six turns for eight waves, 3.5 us with them, 3.1 without; 4 tokens, 2 of 8 experts, 1408 x 1024 gated 9.2 and 7.3).
+// issue all the same (77 x 768 x 768, six turns for eight waves, 3.5 us with them, 3.1 without; 4 tokens, 2 of 8 experts, 2816 x 1024 gated 9.2 and 7.3).
 template <int AHEAD, bool GROUPED, bool GATED> __global__ __launch_bounds__(512) void ft_i8_stream(I8Args a) {
     constexpr int W = 8, NB = GATED ? 2 : 1;
     __shared__ i8_i32x4 sums[W][NB][64];
