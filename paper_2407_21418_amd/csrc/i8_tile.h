@@ -124,7 +124,7 @@ template <int TM, int TN, bool GROUPED> struct I8Tiles {
                 t.row0 = r.beg + row * TM;
                 t.rows = rows < (uint32_t)TM ? rows : (uint32_t)TM;
                 t.n0 = col * TN;
-                t.some = col < a.col_tiles;                  // (offsets that are not ascending can say otherwise)
+                t.some = n_tiles != 0u && col < a.col_tiles; // (offsets that are not ascending can say otherwise, and sums of many such wrap)
                 return t;
             }
             before += __builtin_amdgcn_readlane(here, 63);
