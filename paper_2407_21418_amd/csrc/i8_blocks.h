@@ -74,6 +74,15 @@ inline bool i8_grid(I8Args &a, uint32_t tm, uint32_t tn, bool grouped) {
     return true;
 }
 
+// Where the t-th turn of `groups` k-tiles, one for each group of waves, begins.  `first`: through a long reduce axis every XCD goes from another of its `whole`
+// whole turns on, and round to there (a last turn that the axis ends inside stays the last one).  This is the copies' scalar offset, always inside the axis; the
+// groups' tiles of a turn are 128 bytes apart in the lanes' offsets, so that one beyond the axis is held to the buffer's bound: that is compared with the
+// lanes' offsets, less the scalar one, which must not pass it (a tile of one row can end before the second group's last tile begins).
+constexpr uint32_t i8_turn_begin(uint32_t t, uint32_t groups, uint32_t first, uint32_t whole) {
+    const uint32_t x = t + first;
+    return (t >= whole ? t : x >= whole ? x - whole : x) * groups * 128u;
+}
+
 ft_status i8_launch_blocks(I8Kind kind, bool grouped, I8Args &a, void *stream);
 
 }  // namespace ftk

@@ -113,40 +113,36 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
         I8Columns<TN, GATED> cols;
         uint32_t off_a[LA], off_b[LB];
         uint32_t first_k, whole_k;
-        // (wave: in its group; t: a group's k-tile, which is the block's k-tile GK * t + group)
-        __device__ __forceinline__ Source(const I8Args &g, const I8Tile &tile, const CopyRows &rows, uint32_t wave, uint32_t lane) : cols(g, tile) {
+        // (wave: in its group; a group's t-th k-tile is the block's GK * t + group)
+        __device__ __forceinline__ Source(const I8Args &g, const I8Tile &tile, const CopyRows &rows, uint32_t wave, uint32_t group, uint32_t lane) : cols(g, tile) {
             whole_k = g.k / (128u * GK);
             first_k = g.k >= 8192u ? (blockIdx.x & 7u) * whole_k / 8u : 0u;
             a = GROUPED ? i8_rsrc(g.A, g.a_rows * g.lda) : i8_rsrc(g.A + (uint64_t)tile.row0 * g.lda, tile.rows * g.lda);
 #pragma unroll
             for (int i = 0; i < LA; ++i) {
-                const uint32_t row = wave * (LA * 8) + i * 8 + lane / 8u, kc = (lane & 7u) ^ i8_swizzle(row);
-                if constexpr (GROUPED) off_a[i] = rows.of_a[i] == ~0u ? kOutside : rows.of_a[i] * g.lda + kc * 16u;
-                else off_a[i] = row * g.lda + kc * 16u;
+                const uint32_t row = wave * (LA * 8) + i * 8 + lane / 8u, kc = (lane & 7u) ^ i8_swizzle(row), at = group * 128u + kc * 16u;
+                if constexpr (GROUPED) off_a[i] = rows.of_a[i] == ~0u ? kOutside : rows.of_a[i] * g.lda + at;
+                else off_a[i] = row * g.lda + at;
             }
 #pragma unroll
             for (int i = 0; i < LB; ++i) {
                 const uint32_t row = wave * (LB * 8) + i * 8 + lane / 8u, kc = (lane & 7u) ^ i8_swizzle(row);
-                off_b[i] = ((GATED ? row / 32u * 16u + (row & 15u) : row) * g.ldb) + kc * 16u;
+                off_b[i] = ((GATED ? row / 32u * 16u + (row & 15u) : row) * g.ldb) + group * 128u + kc * 16u;
             }
         }
-        // Where the t-th k-tile that is taken begins.  Through a long reduce axis every XCD goes from another place on, and round to there (a last k-tile that
-        // the axis ends inside stays the last one): they do not all ask for the same part of the same rows then.  128 x 256: 2048 x 4096 x 11008 89 us all
-        // from the beginning, 85.5 so, 2048 x 5120 x 13824 180 and 173, 2048 x 4096 x 4096 32 both; 256 x 256 has no scalar instructions to spare in
-        // its loop: 8192 x 8192 x 8192 396 and 404.
-        __device__ __forceinline__ uint32_t at_k(uint32_t t, uint32_t group) const {
-            if constexpr (!SLOTS) {
-                const uint32_t x = t + first_k;
-                t = t >= whole_k ? t : x >= whole_k ? x - whole_k : x;
-            }
-            return t * (128u * GK) + group * 128u;
+        // Where the t-th turn's k-tiles begin: from another place on for every XCD where the reduce axis is long, so that they do not all ask for the same
+        // part of the same rows.  128 x 256: 2048 x 4096 x 11008 89 us all from the beginning, 85.5 so, 2048 x 5120 x 13824 180 and 173, 2048 x 4096 x 4096 32
+        // both; 256 x 256 has no scalar instructions to spare in its loop: 8192 x 8192 x 8192 396 and 404.
+        __device__ __forceinline__ uint32_t at_k(uint32_t t) const {
+            if constexpr (SLOTS) return t * 128u;
+            return i8_turn_begin(t, GK, first_k, whole_k);
         }
-        template <int I> __device__ __forceinline__ void copy_a(unsigned char *smem, uint32_t wave, uint32_t group, uint32_t t, uint32_t slot) const {
-            i8_copy(a, smem + slot + wave * (LA * 1024) + I * 1024, off_a[I], at_k(t, group));
+        template <int I> __device__ __forceinline__ void copy_a(unsigned char *smem, uint32_t wave, uint32_t t, uint32_t slot) const {
+            i8_copy(a, smem + slot + wave * (LA * 1024) + I * 1024, off_a[I], at_k(t));
         }
-        template <int I> __device__ __forceinline__ void copy_b(unsigned char *smem, uint32_t wave, uint32_t group, uint32_t t, uint32_t slot) const {
+        template <int I> __device__ __forceinline__ void copy_b(unsigned char *smem, uint32_t wave, uint32_t t, uint32_t slot) const {
             const bool values = GATED && (((wave * (LB * 8) + I * 8) / 16u) & 1u);
-            i8_copy(values ? cols.values : cols.b, smem + slot + wave * (LB * 1024) + I * 1024, off_b[I], at_k(t, group));
+            i8_copy(values ? cols.values : cols.b, smem + slot + wave * (LB * 1024) + I * 1024, off_b[I], at_k(t));
         }
     };
     static __device__ __forceinline__ uint32_t next_slot(uint32_t s) {
@@ -154,13 +150,13 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
         return s + STEP >= (uint32_t)RING ? s + STEP - RING : s + STEP;
     }
     // the ring full
-    static __device__ __forceinline__ void fill(const Source &src, unsigned char *ring, uint32_t wave, uint32_t group, uint32_t nk) {
+    static __device__ __forceinline__ void fill(const Source &src, unsigned char *ring, uint32_t wave, uint32_t nk) {
         uint32_t pa = 0, pb = A_BYTES;
 #pragma unroll
         for (int t = 0; t < FAR; ++t) {
             if ((uint32_t)t < nk) {
-                i8_each<0, LA>([&](auto i) { src.template copy_a<decltype(i)::value>(ring, wave, group, t, pa); });
-                if (!SLOTS || t < 2) i8_each<0, LB>([&](auto i) { src.template copy_b<decltype(i)::value>(ring, wave, group, t, pb); });
+                i8_each<0, LA>([&](auto i) { src.template copy_a<decltype(i)::value>(ring, wave, t, pa); });
+                if (!SLOTS || t < 2) i8_each<0, LB>([&](auto i) { src.template copy_b<decltype(i)::value>(ring, wave, t, pb); });
             }
             pa = next_slot(pa); pb = next_slot(pb);
         }
@@ -212,13 +208,13 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
         if (!tile.some) return;
         CopyRows rows;
         rows.ask(g, tile, wave, lane);
-        Source src(g, tile, rows, wave, lane);
+        Source src(g, tile, rows, wave, group, lane);
         Finals fin;
         if constexpr (EARLY) {
             fin.sources(g, tile, wave, group, lane);
             fin.ask(g, tile, src.cols, wave, group, lane);
         }
-        fill(src, ring, wave, group, nk);
+        fill(src, ring, wave, nk);
         for (uint32_t turn = 1;; ++turn) {
             i8_i32x4 acc[BM][BN];
 #pragma unroll
@@ -232,7 +228,7 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
             }
             // a wave whose part of the tile lies beyond the last row or column copies for the others, and leaves them the matrix cores
             const bool idle = (wave / GN) * WM >= tile.rows || src.cols.first + (wave % GN) * (WN / PER) >= src.cols.of_c;
-            if (idle) copies_alone(src, ring, wave, group, nk, turn > 1 && counted(g));
+            if (idle) copies_alone(src, ring, wave, nk, turn > 1 && counted(g));
             else products(g, src, ring, wave, group, lane, nk, turn > 1 && counted(g), acc);
             const I8Tile done = tile;
             const I8Columns<TN, GATED> cols = src.cols;
@@ -247,8 +243,8 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
             if (next.some) {
                 // (every wave has read the last k-tile: they met after its second k-step had arrived)
                 if constexpr (GK > 1) __syncthreads();               // the sums have been read
-                src = Source(g, next, rows, wave, l);
-                fill(src, ring, wave, group, nk);
+                src = Source(g, next, rows, wave, group, l);
+                fill(src, ring, wave, nk);
                 __builtin_amdgcn_sched_barrier(0);
             }
             if constexpr (GK > 1) results(g, done, cols, fin, l, kept);
@@ -300,27 +296,27 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
         __builtin_amdgcn_s_barrier();
     }
     // the Q-th of the copies that are due once tile t has been read
-    template <int Q, bool STEADY> static __device__ __forceinline__ void copy_behind(const Source &src, unsigned char *ring, uint32_t wave, uint32_t group, uint32_t t, uint32_t nk, uint32_t sa, uint32_t sb) {
+    template <int Q, bool STEADY> static __device__ __forceinline__ void copy_behind(const Source &src, unsigned char *ring, uint32_t wave, uint32_t t, uint32_t nk, uint32_t sa, uint32_t sb) {
         if constexpr (SLOTS) {
-            if constexpr (Q < LB) { if (STEADY || t + 2u < nk) src.template copy_b<Q>(ring, wave, group, t + 2u, sa); }
-            else if constexpr (STEADY) src.template copy_a<Q - LB>(ring, wave, group, t + 3u, sb);
+            if constexpr (Q < LB) { if (STEADY || t + 2u < nk) src.template copy_b<Q>(ring, wave, t + 2u, sa); }
+            else if constexpr (STEADY) src.template copy_a<Q - LB>(ring, wave, t + 3u, sb);
         } else if constexpr (STEADY) {
-            if constexpr (Q < LA) src.template copy_a<Q>(ring, wave, group, t + STAGES, sa);
-            else src.template copy_b<Q - LA>(ring, wave, group, t + STAGES, sb);
+            if constexpr (Q < LA) src.template copy_a<Q>(ring, wave, t + STAGES, sa);
+            else src.template copy_b<Q - LA>(ring, wave, t + STAGES, sb);
         }
     }
 
-    __device__ static __forceinline__ void copies_alone(const Source &src, unsigned char *ring, uint32_t wave, uint32_t group, uint32_t nk, bool stores) {
+    __device__ static __forceinline__ void copies_alone(const Source &src, unsigned char *ring, uint32_t wave, uint32_t nk, bool stores) {
         uint32_t sa = 0, sb = A_BYTES, t = 0;
         first_landed(nk, stores);
         for (; t + FAR < nk; ++t) {
             next_landed<true>(t, nk);
-            i8_each<0, LA + LB>([&](auto q) { copy_behind<decltype(q)::value, true>(src, ring, wave, group, t, nk, sa, sb); });
+            i8_each<0, LA + LB>([&](auto q) { copy_behind<decltype(q)::value, true>(src, ring, wave, t, nk, sa, sb); });
             sa = next_slot(sa); sb = next_slot(sb);
         }
         for (; t < nk; ++t) {
             next_landed<false>(t, nk);
-            i8_each<0, LA + LB>([&](auto q) { copy_behind<decltype(q)::value, false>(src, ring, wave, group, t, nk, sa, sb); });
+            i8_each<0, LA + LB>([&](auto q) { copy_behind<decltype(q)::value, false>(src, ring, wave, t, nk, sa, sb); });
             sa = next_slot(sa); sb = next_slot(sb);
         }
     }
@@ -364,7 +360,7 @@ template <int WM, int WN, int GM, int GN, int GK, int STAGES, bool GROUPED, bool
             __builtin_amdgcn_sched_barrier(0);
             const uint32_t na = next_slot(sa), nb = next_slot(sb);
             // (past the last tile the reads fetch what happens to be there, for nobody)
-            phase<0, SLOTS || STEADY>(fa + na, fb + nb, f0, f1, acc, [&](auto q) { copy_behind<decltype(q)::value, STEADY>(src, ring, wave, group, t, nk, sa, sb); });
+            phase<0, SLOTS || STEADY>(fa + na, fb + nb, f0, f1, acc, [&](auto q) { copy_behind<decltype(q)::value, STEADY>(src, ring, wave, t, nk, sa, sb); });
             sa = na; sb = nb;
         };
         uint32_t t = 0;

@@ -1,0 +1,61 @@
+"""Where matmuls in 8-bit integers and moves of tokens reach, by the rules of their launches compiled for the CPU (g++): copies that begin inside their rows."""
+import ctypes as C
+import os
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+SOURCE = r"""
+#include "i8_blocks.h"
+extern "C" int kernel(unsigned m, unsigned n, unsigned k, int gated, int experts) {
+    ftk::I8Args a{};
+    a.m = m; a.n = n; a.k = k; a.gated = gated; a.experts = experts; a.cus = 256;
+    return (int)ftk::i8_choose(a, experts > 0);
+}
+// the first turn whose scalar offset is at or beyond the reduce axis' end, or that reads other tiles than all of them once; -1: none
+extern "C" int bad_turn(unsigned k, unsigned groups, unsigned xcd, int rotated) {
+    const unsigned tiles = (k + 127u) / 128u, nk = (tiles + groups - 1u) / groups, whole = k / (128u * groups), first = rotated ? xcd * whole / 8u : 0u;
+    static unsigned char seen[4096];
+    for (unsigned i = 0; i < tiles; ++i) seen[i] = 0;
+    for (unsigned t = 0; t < nk; ++t)
+        for (unsigned g = 0; g < groups; ++g) {
+            const unsigned begin = ftk::i8_turn_begin(t, groups, first, whole), at = begin + g * 128u;
+            if (begin >= k || at % 128u) return (int)t;
+            if (at < k && seen[at / 128u]++) return (int)t;
+            if (t >= whole && begin != t * groups * 128u) return (int)t;          // (where the axis ends inside: the tiles that are cut)
+        }
+    for (unsigned i = 0; i < tiles; ++i)
+        if (!seen[i]) return (int)nk;
+    return -1;
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def rules(tmp_path_factory):
+    if not shutil.which("g++"):
+        pytest.skip("no g++")
+    at = tmp_path_factory.mktemp("ranges")
+    (at / "rules.cpp").write_text(SOURCE)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", os.path.join(ROOT, "paper_2407_21418_amd", "csrc"), str(at / "rules.cpp"),
+                    "-o", str(at / "rules.so")], check=True)
+    return C.CDLL(str(at / "rules.so"))
+
+
+@pytest.mark.parametrize("groups", [1, 2])
+def test_copies_begin_inside_the_reduce_axis(rules, groups):
+    """A tile of one row is read up to its pitch, k rounded up to 16 bytes, and a buffer's bound holds the lanes' offsets alone: the scalar one has to stay before it."""
+    for k in list(range(1, 2100)) + [4096, 4100, 8191, 8192, 8193, 8300, 8449, 11008, 65537, 131071]:
+        for xcd in range(8 if k >= 8192 else 1):
+            assert rules.bad_turn(k, groups, xcd, int(k >= 8192)) == -1, (k, xcd)
+
+
+# blocks of 64 x 64, two groups along the reduce axis, whose last rows and columns of blocks have one row or column, with an odd number of k-tiles: m, n, k, experts
+ONE_ROW = [(65, 2049, 4100, 0), (129, 2049, 8310, 0), (33, 777, 4100, 7)]
+
+
+def test_blocks_of_one_row(rules):
+    for m, n, k, experts in ONE_ROW:
+        assert rules.kernel(m, n, k, 0, experts) == 1 and (k + 127) // 128 % 2 == 1 and (experts or m % 64 == 1) and (n % 64 == 1 or experts), (m, n, k, experts)
