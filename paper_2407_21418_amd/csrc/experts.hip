@@ -196,11 +196,11 @@ template <int V> struct MovePiece {
 
 // The rows of entries j0 .. of token t, ~0 where there is none
 template <int DT> __device__ __forceinline__ void entries_of(const MoveArgs &a, uint32_t t, uint32_t j0, uint32_t (&row)[kEntries]) {
-    const uint32_t n = a.top_k - j0 < (uint32_t)kEntries ? a.top_k - j0 : (uint32_t)kEntries, most = a.tokens * a.top_k;
+    const uint32_t n = a.top_k - j0 < (uint32_t)kEntries ? a.top_k - j0 : (uint32_t)kEntries;
 #pragma unroll
     for (int j = 0; j < kEntries; ++j) {
         row[j] = (uint32_t)j < n ? (uint32_t)a.row_of[(uint64_t)t * a.top_k + j0 + j] : ~0u;
-        if (row[j] >= most) row[j] = ~0u;
+        if (row[j] >= a.entries) row[j] = ~0u;
     }
 }
 
@@ -367,27 +367,37 @@ enum { MOVE_GATHER, MOVE_COMBINE, MOVE_GRAD };
 // Rows beyond what the last-level cache holds (256 MB) are streamed: 8192 tokens x 8 of 4096 bf16, all moves of a training step 640 us kept, 566
 // streamed; 1234 x 6 of 1001 fp16 the rows stay for the next call: combine 7.0 us kept, 8.4 streamed.
 constexpr uint64_t kStreamBytes = 256ull << 20;
-template <int DT, bool STREAM> void move_launch(int what, const MoveArgs &a, hipStream_t stream) {
+template <int DT, bool STREAM> ft_status move_launch(int what, MoveArgs a, hipStream_t stream) {
     const MoveShape s = move_shape<DT>(a);
-    const uint32_t per = 256u / s.lanes;
-    const dim3 grid((uint32_t)(((uint64_t)a.tokens + per - 1u) / per)), block(256);
-    if (what == MOVE_GATHER) hipLaunchKernelGGL((ft_expert_gather_kernel<DT, STREAM>), grid, block, 0, stream, a, s);
-    else if (what == MOVE_COMBINE) hipLaunchKernelGGL((ft_expert_combine_kernel<DT, STREAM>), grid, block, 0, stream, a, s);
-    else if (a.dweights) hipLaunchKernelGGL((ft_expert_grad_kernel<DT, true, STREAM>), grid, block, 0, stream, a, s);
-    else hipLaunchKernelGGL((ft_expert_grad_kernel<DT, false, STREAM>), grid, block, 0, stream, a, s);
+    const uint32_t per = 256u / s.lanes, most = launch_rows(per, 256u);
+    for (;; a.tokens -= most) {
+        MoveArgs part = a;
+        if (part.tokens > most) part.tokens = most;
+        const dim3 grid((part.tokens + per - 1u) / per), block(256);
+        if (what == MOVE_GATHER) hipLaunchKernelGGL((ft_expert_gather_kernel<DT, STREAM>), grid, block, 0, stream, part, s);
+        else if (what == MOVE_COMBINE) hipLaunchKernelGGL((ft_expert_combine_kernel<DT, STREAM>), grid, block, 0, stream, part, s);
+        else if (a.dweights) hipLaunchKernelGGL((ft_expert_grad_kernel<DT, true, STREAM>), grid, block, 0, stream, part, s);
+        else hipLaunchKernelGGL((ft_expert_grad_kernel<DT, false, STREAM>), grid, block, 0, stream, part, s);
+        const ft_status st = op_launched();
+        if (st != FT_OK || a.tokens <= most) return st;
+        const uint64_t bytes = (uint64_t)most * a.ld_token * RowType<DT>::BYTES, entries = (uint64_t)most * a.top_k;
+        if (what == MOVE_COMBINE) a.dst = static_cast<unsigned char *>(a.dst) + bytes;
+        else a.src = static_cast<const unsigned char *>(a.src) + bytes;
+        a.row_of += entries;
+        if (a.weights) a.weights += entries;
+        if (a.dweights) a.dweights += entries;
+    }
 }
-template <int DT> void move_launch(int what, const MoveArgs &a, hipStream_t stream) {
-    if ((uint64_t)a.tokens * a.top_k * a.cols * RowType<DT>::BYTES > kStreamBytes) move_launch<DT, true>(what, a, stream);
-    else move_launch<DT, false>(what, a, stream);
+template <int DT> ft_status move_launch(int what, const MoveArgs &a, hipStream_t stream) {
+    return (uint64_t)a.entries * a.cols * RowType<DT>::BYTES > kStreamBytes ? move_launch<DT, true>(what, a, stream) : move_launch<DT, false>(what, a, stream);
 }
 ft_status move(int what, const ft_expert_desc *desc, const MoveArgs &a, void *stream) {
     const ft_status st = op_stream_check(stream);
     if (st != FT_OK) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (desc->dtype == FT_F16) move_launch<ROW_F16>(what, a, s);
-    else if (desc->dtype == FT_BF16) move_launch<ROW_BF16>(what, a, s);
-    else move_launch<ROW_F32>(what, a, s);
-    return op_launched();
+    if (desc->dtype == FT_F16) return move_launch<ROW_F16>(what, a, s);
+    if (desc->dtype == FT_BF16) return move_launch<ROW_BF16>(what, a, s);
+    return move_launch<ROW_F32>(what, a, s);
 }
 
 }  // namespace

@@ -12,6 +12,10 @@ inline bool aligned_to(const void *p, uintptr_t bytes) { return reinterpret_cast
 
 constexpr uint32_t kMaxExperts = 1024, kMaxTopK = 32, kMaxCols = 1u << 20, kMaxK = 131071;
 
+// A launch has fewer than 2^32 threads: rows, `per` of them to a workgroup of `threads`, that one can take.  More rows are several launches.
+constexpr uint32_t kMostThreads = 0xffffffffu;
+constexpr uint32_t launch_rows(uint32_t per, uint32_t threads) { return kMostThreads / threads * per; }
+
 // ---- quantised rows ----
 struct QuantArgs {
     const void *X;
@@ -131,6 +135,7 @@ struct MoveArgs {
     const float *weights;
     float *dweights;
     uint32_t tokens, top_k, cols, ld_token, ld_row;
+    uint32_t entries;                    // of all launches of a call: rows of Y and dY
 };
 // what the three calls share; the caller has set the pointers of `a`
 inline ft_status move_check(const ft_expert_desc *d, uint32_t tokens, bool need_other, MoveArgs *a, bool *launch) {
@@ -140,6 +145,7 @@ inline ft_status move_check(const ft_expert_desc *d, uint32_t tokens, bool need_
     if (d->cols == 0 || d->dtype > FT_F32) return FT_ERR_INVALID_ARG;
     if (d->cols > kMaxCols) return FT_ERR_UNSUPPORTED;
     a->tokens = tokens; a->top_k = d->top_k; a->cols = d->cols;
+    a->entries = tokens * d->top_k;
     a->ld_token = d->ld_token ? d->ld_token : d->cols;
     a->ld_row = d->ld_row ? d->ld_row : d->cols;
     if (a->ld_token < d->cols || a->ld_row < d->cols) return FT_ERR_INVALID_ARG;

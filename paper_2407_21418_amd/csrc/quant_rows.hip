@@ -170,7 +170,7 @@ using namespace ftk;
 
 namespace {
 
-template <int DT, bool GATED> void launch(const QuantArgs &a, hipStream_t s) {
+template <int DT, bool GATED> ft_status launch(QuantArgs a, hipStream_t s) {
     // Pieces of a thread: one where a few rows leave the device idle (16 x 4096 bf16 3.0 us, with two 3.25; from 1024 rows on alike), four where
     // more in flight is what wide rows lack (8192 x 4096 bf16 20.8 us, with two 22.1; 8192 x 11008 48.9 and 50.9), else two (65536 x 1408 fp32
     // 81.0 us, with four 83.2; 2048 x 2 x 11008 gated 24.0 and 25.8; 8192 x 2048 bf16 12.7 and 13.6).
@@ -179,11 +179,21 @@ template <int DT, bool GATED> void launch(const QuantArgs &a, hipStream_t s) {
     uint32_t threads = ((pieces + hold - 1u) / hold + 63u) / 64u * 64u;
     if (threads > 1024u) threads = 1024u;
     const uint32_t per = threads == 64u ? 4u : 1u;
-    const dim3 grid((a.rows + per - 1u) / per), block(threads * per);
-    if (pieces <= threads) hipLaunchKernelGGL((ft_quant<DT, GATED, 1>), grid, block, 0, s, a, threads);
-    else if (pieces <= 2u * threads) hipLaunchKernelGGL((ft_quant<DT, GATED, 2>), grid, block, 0, s, a, threads);
-    else if (pieces <= 4u * threads) hipLaunchKernelGGL((ft_quant<DT, GATED, 4>), grid, block, 0, s, a, threads);
-    else hipLaunchKernelGGL((ft_quant<DT, GATED, 0>), grid, block, 0, s, a, threads);
+    const uint32_t most = launch_rows(per, threads * per);
+    for (;; a.rows -= most) {
+        QuantArgs part = a;
+        if (part.rows > most) part.rows = most;
+        const dim3 grid((part.rows + per - 1u) / per), block(threads * per);
+        if (pieces <= threads) hipLaunchKernelGGL((ft_quant<DT, GATED, 1>), grid, block, 0, s, part, threads);
+        else if (pieces <= 2u * threads) hipLaunchKernelGGL((ft_quant<DT, GATED, 2>), grid, block, 0, s, part, threads);
+        else if (pieces <= 4u * threads) hipLaunchKernelGGL((ft_quant<DT, GATED, 4>), grid, block, 0, s, part, threads);
+        else hipLaunchKernelGGL((ft_quant<DT, GATED, 0>), grid, block, 0, s, part, threads);
+        const ft_status st = op_launched();
+        if (st != FT_OK || a.rows <= most) return st;
+        a.X = static_cast<const unsigned char *>(a.X) + (uint64_t)most * a.ldx * RowType<DT>::BYTES;
+        a.Q += (uint64_t)most * a.ldq;
+        a.scale += most;
+    }
 }
 
 }  // namespace
@@ -196,8 +206,7 @@ extern "C" ft_status ft_i8_quantize(const ft_quant_desc *desc, uint32_t rows, co
     if (st != FT_OK || !go) return st;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const bool gated = desc->act == FT_ACT_SILU_MUL;
-    if (desc->dtype == FT_F16) gated ? launch<ROW_F16, true>(a, s) : launch<ROW_F16, false>(a, s);
-    else if (desc->dtype == FT_BF16) gated ? launch<ROW_BF16, true>(a, s) : launch<ROW_BF16, false>(a, s);
-    else gated ? launch<ROW_F32, true>(a, s) : launch<ROW_F32, false>(a, s);
-    return op_launched();
+    if (desc->dtype == FT_F16) return gated ? launch<ROW_F16, true>(a, s) : launch<ROW_F16, false>(a, s);
+    if (desc->dtype == FT_BF16) return gated ? launch<ROW_BF16, true>(a, s) : launch<ROW_BF16, false>(a, s);
+    return gated ? launch<ROW_F32, true>(a, s) : launch<ROW_F32, false>(a, s);
 }

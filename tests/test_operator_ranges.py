@@ -1,4 +1,5 @@
-"""Where matmuls in 8-bit integers and moves of tokens reach, by the rules of their launches compiled for the CPU (g++): copies that begin inside their rows."""
+"""Where matmuls in 8-bit integers and moves of tokens reach, by the rules of their launches compiled for the CPU (g++): copies that begin inside their rows,
+launches that HIP takes."""
 import ctypes as C
 import os
 import shutil
@@ -14,6 +15,7 @@ extern "C" int kernel(unsigned m, unsigned n, unsigned k, int gated, int experts
     a.m = m; a.n = n; a.k = k; a.gated = gated; a.experts = experts; a.cus = 256;
     return (int)ftk::i8_choose(a, experts > 0);
 }
+extern "C" unsigned most_rows(unsigned per, unsigned threads) { return ftk::launch_rows(per, threads); }
 // the first turn whose scalar offset is at or beyond the reduce axis' end, or that reads other tiles than all of them once; -1: none
 extern "C" int bad_turn(unsigned k, unsigned groups, unsigned xcd, int rotated) {
     const unsigned tiles = (k + 127u) / 128u, nk = (tiles + groups - 1u) / groups, whole = k / (128u * groups), first = rotated ? xcd * whole / 8u : 0u;
@@ -59,3 +61,9 @@ ONE_ROW = [(65, 2049, 4100, 0), (129, 2049, 8310, 0), (33, 777, 4100, 7)]
 def test_blocks_of_one_row(rules):
     for m, n, k, experts in ONE_ROW:
         assert rules.kernel(m, n, k, 0, experts) == 1 and (k + 127) // 128 % 2 == 1 and (experts or m % 64 == 1) and (n % 64 == 1 or experts), (m, n, k, experts)
+
+
+@pytest.mark.parametrize("per,threads", [(4, 256), (1, 64), (1, 128), (1, 960), (1, 1024)] + [(256 // lanes, 256) for lanes in (8, 16, 32, 64, 128, 256)])
+def test_launches_have_fewer_than_2_to_the_32_threads(rules, per, threads):
+    most = rules.most_rows(per, threads) % (1 << 32)
+    assert most % per == 0 and most // per * threads < 1 << 32 <= (most // per + 1) * threads
