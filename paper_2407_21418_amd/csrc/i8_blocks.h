@@ -41,12 +41,12 @@ inline float i8_time(const I8Args &a, I8Kind kind, bool grouped) {
     const I8KindInfo i = i8_kind_info(kind, a.gated != 0);
     const float row_tiles = i8_row_tiles(a, i.tm, grouped), tiles = row_tiles * (float)((a.n + i.tn - 1u) / i.tn), share = tiles / (float)(a.cus * i.per_cu);
     const float k = (float)((a.k + 127u) / 128u);
-    float rounds = (float)(uint32_t)share;
+    float rounds = (float)(uint64_t)share;
     if (rounds < share) rounds += 1.f;
     // By expert a tile first reads where its rows lie, then their numbers: a microsecond more.  Blocks ask for the next tile's ahead; the first kind
     // waits anew once for what a CU holds, four workgroups, two with gates (4 tokens, 2 of 16 experts, 2816 x 2048 gated: 11.0 us in three
     // rounds of the first kind, 10.5 in one of the third, which are expected at 8.5 and 9.8 without this).
-    const float held = kind == I8_STREAM ? (a.gated ? 2.f : 4.f) : rounds, waits = grouped ? (float)(uint32_t)((rounds + held - 1.f) / held) : 0.f;
+    const float held = kind == I8_STREAM ? (a.gated ? 2.f : 4.f) : rounds, waits = grouped ? (float)(uint64_t)((rounds + held - 1.f) / held) : 0.f;
     // ... and each row of tiles reads its expert's weights, which other rows of tiles seldom find in the caches: 10 us a GB (32 products of 256 .. 65536
     // entries and 8 .. 64 experts, all kinds measured: the chosen one is 1.3 % slower than the fastest on average, without this term 3.1 %).
     const float weights = grouped ? 1e-8f * row_tiles * (float)a.n * (float)a.k : 0.f;

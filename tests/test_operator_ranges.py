@@ -67,3 +67,19 @@ def test_blocks_of_one_row(rules):
 def test_launches_have_fewer_than_2_to_the_32_threads(rules, per, threads):
     most = rules.most_rows(per, threads) % (1 << 32)
     assert most % per == 0 and most // per * threads < 1 << 32 <= (most // per + 1) * threads
+
+
+def test_the_first_kernel_s_launches_too(rules):
+    """Its workgroups of 512 threads have a tile of 16 x 16 each, 16 x 32 with gates; the other kernels' take the tiles in turn."""
+    for bits in range(20, 32):
+        for m in (1 << bits) - 1, 5 << (bits - 3):
+            if m >= 1 << 31:
+                continue
+            for n in [1 << b for b in range(20)] + [3, 17, 24, 48, 80, 1000, (1 << 20) - 2]:
+                for k in (1, 128, 129, 512, 4096, 131071):
+                    for gates in (0, 1):
+                        if n % 2 and gates:
+                            continue
+                        for experts in (0, 1, 64, 1024):
+                            tiles = (m // 16 + experts if experts else -(-m // 16)) * -(-n // (32 if gates else 16))
+                            assert tiles * 512 < 1 << 32 or rules.kernel(m, n, k, gates, experts) > 0, (m, n, k, gates, experts)
