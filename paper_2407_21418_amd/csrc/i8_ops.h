@@ -74,7 +74,7 @@ inline ft_status i8_check(const ft_i8_desc *d, bool grouped, uint32_t m, const i
     a->ldc = d->ldc ? d->ldc : columns;
     if (a->lda < d->k || a->ldb < d->k || a->ldc < columns || a->lda % 16u || a->ldb % 16u) return FT_ERR_INVALID_ARG;
     if (a->lda > (1u << 20) || a->ldb > (1u << 20) || a->ldc > (1u << 22)) return FT_ERR_UNSUPPORTED;
-    if (grouped && (uint64_t)a_rows * a->lda >= 0x7fff0000ull) return FT_ERR_UNSUPPORTED;
+    if (grouped && (uint64_t)a_rows * a->lda >= 0x80000000ull) return FT_ERR_UNSUPPORTED;
     if ((d->epilogue == FT_EPI_BIAS) != (bias != nullptr)) return FT_ERR_INVALID_ARG;
     if (m == 0) return FT_OK;
     a->out_kind = d->out_dtype == FT_OUT_F32 ? 0u : d->dtype == FT_F16 ? 1u : 2u;

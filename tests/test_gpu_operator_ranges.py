@@ -100,3 +100,24 @@ def test_products_of_more_rows_than_threads_for_them(m, n, k, experts):
             rows = slice(at, min(offsets[e + 1], at + (1 << 22)))
             ref, size = p.exact(0, a_row[rows].long() if experts else rows, e)
             check(c[rows], ref, size, "f16")
+
+
+@pytest.mark.parametrize("rows,n", [(16, 80), (1300, 2064)])
+def test_the_last_rows_of_2_gb(rows, n):
+    """a_rows * lda just below 2^31: the last rows of A, and rows that it does not have."""
+    lda, a_rows, k = 16384, 131071, 300
+    p = Problem(1, n, k, experts=2)
+    p.a, p.lda, p.sa = torch.zeros(a_rows, lda, dtype=torch.int8, device="cuda"), lda, torch.rand(a_rows, device="cuda") + 0.1
+    p.a[-rows:] = torch.randint(-128, 128, (rows, lda), generator=torch.Generator(device="cuda").manual_seed(4), device="cuda", dtype=torch.int8)
+    source = torch.arange(a_rows - 1, a_rows - 1 - rows, -1, device="cuda")
+    a_row = source.int()
+    a_row[0], a_row[1] = a_rows, -1
+    offsets = torch.tensor([0, rows // 3, rows], dtype=torch.int32, device="cuda")
+    c = torch.full((rows, n), 7.0, device="cuda")
+    ft.ft_i8_matmul_experts(p.desc("f32", experts=2), rows, offsets.data_ptr(), p.a.data_ptr(), p.sa.data_ptr(), a_row.data_ptr(), a_rows, p.b.data_ptr(), p.sb.data_ptr(), 0, c.data_ptr(), stream())
+    torch.cuda.synchronize()
+    for e, at in enumerate((slice(0, rows // 3), slice(rows // 3, rows))):
+        ref, size = p.exact(0, source[at], e)
+        if e == 0:
+            ref[0], ref[1] = 0, 0
+        check(c[at], ref, size, "f32")

@@ -7,6 +7,8 @@ import subprocess
 
 import pytest
 
+import paper_2407_21418_amd as ft
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SOURCE = r"""
 #include "i8_blocks.h"
@@ -83,3 +85,14 @@ def test_the_first_kernel_s_launches_too(rules):
                         for experts in (0, 1, 64, 1024):
                             tiles = (m // 16 + experts if experts else -(-m // 16)) * -(-n // (32 if gates else 16))
                             assert tiles * 512 < 1 << 32 or rules.kernel(m, n, k, gates, experts) > 0, (m, n, k, gates, experts)
+
+
+@pytest.mark.parametrize("lda,a_rows,fits", [(16, (1 << 27) - 1, True), (16, 1 << 27, False), (16384, 131071, True), (16384, 131072, False), (1 << 20, 2047, True), (1 << 20, 2048, False)])
+def test_rows_by_expert_lie_within_2_gb(lda, a_rows, fits):
+    """a_rows * lda < 2^31 (no rows of C: nothing is launched)."""
+    call = lambda: ft.ft_i8_matmul_experts(ft.ft_i8_desc(n=16, k=16, lda=lda, experts=2), 0, 0, 0, 0, 0, a_rows, 0, 0, 0, 0)  # noqa: E731
+    if fits:
+        return call()
+    with pytest.raises(ft.FtError) as e:
+        call()
+    assert e.value.status == ft.FT_ERR_UNSUPPORTED
