@@ -476,7 +476,8 @@ enum { FT_ACT_NONE = 0, FT_ACT_SILU_MUL = 1 };
 enum { FT_EPI_SILU_MUL = 2 };      /* epilogue of ft_i8_desc only                            */
 
 /* Rows of values as 8-bit integers with one scale each.  f = X[i, 0 .. cols), or with FT_ACT_SILU_MUL
- * f[j] = g / (1 + exp(-g)) * u for g = X[i, j], u = X[i, cols + j] (in fp32, not rounded to 16 bits):
+ * f[j] = g / (1 + exp(-g)) * u for g = X[i, j], u = X[i, cols + j] (in fp32, not rounded to 16 bits; zero for
+ * finite u and finite g below -88.72, whose exp(-g) is beyond fp32):
  *   scale[i] = max_j |f[j]| / 127,  Q[i, j] = 127 f[j] / max_j |f[j]| rounded to nearest, ties to even
  * -- exactly so for 16-bit values without an activation; else in fp32, so that a value beside the middle
  * between two integers may be one off.  A row of zeros has scale 0 and zeros; a row that holds an infinity or a NaN (or
@@ -500,7 +501,7 @@ ft_status ft_i8_quantize(const ft_quant_desc *desc, uint32_t rows, const void *X
  *   C[i, j] = scale_a[i] * scale_b[j] * sum_k A[i, k] B[j, k] (+ bias[j])
  * B is stored [N][K] (FT_B_NK).  The sum is an exact 32-bit integer (k <= 131071), the rest is fp32, rounded once where C has 16 bits.
  * With FT_EPI_SILU_MUL the n columns are n / 2 gates and n / 2 values, and C has n / 2 columns: C[i, j] = g / (1 + exp(-g)) * p[i, n / 2 + j] for
- * the products p above and g = p[i, j].  A C of 16 bits that is quantised again, with or without an activation, loses several times its own rounding: the integers
+ * the products p above and g = p[i, j], in fp32 as there.  A C of 16 bits that is quantised again, with or without an activation, loses several times its own rounding: the integers
  * beside the middle between two fall to another side.  Keep FT_OUT_F32 there. */
 typedef struct ft_i8_desc {
     uint32_t struct_size;

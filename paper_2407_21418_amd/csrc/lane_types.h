@@ -73,8 +73,13 @@ template <int DT> struct RowType {
     }
 };
 
-// g / (1 + exp(-g)) * u.  exp(-g) is 2^(-g log2 e) with the exponent rounded: within (1.22 |g| + 2) 2^-24 of itself, which a gate far below zero, whose
-// result is next to nothing, feels most; a third of the instructions of a call of expf, and infinities and NaNs come out as by the formula.
-__device__ __forceinline__ float silu_mul(float g, float u) { return g * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-0x1.715476p+0f * g)) * u; }
+// g / (1 + exp(-g)) * u.  exp(-g) is 2^(-g log2 e) with the exponent rounded: within (1.22 |g| + 2) 2^-24 of itself, which a gate far below zero
+// feels most; a third of the instructions of a call of expf, and infinities and NaNs come out as by the formula.  The reciprocal is of a quarter of the sum: of
+// one beyond 2^126, for gates below -87.3, the instruction leaves zero, where the result need not be small (-88 times 3e38: -160).  Below -88.72 exp(-g) is
+// infinite, and the result is zero.
+__device__ __forceinline__ float silu_mul(float g, float u) {
+    const float quarter = __builtin_fmaf(0.25f, __builtin_amdgcn_exp2f(-0x1.715476p+0f * g), 0.25f);
+    return g * (0.25f * __builtin_amdgcn_rcpf(quarter)) * u;
+}
 
 }  // namespace ftk
