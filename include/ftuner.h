@@ -521,7 +521,8 @@ ft_status ft_i8_matmul(const ft_i8_desc *desc, uint32_t m, const int8_t *A, cons
                        const float *bias, void *C, void *hip_stream);
 /* The same for rows sorted by expert, in one launch whose group sizes are read on the device: rows offsets[e] .. offsets[e + 1] of C
  * are products with weight e of B [experts][n][ldb], scale_b [experts][n], bias [experts][n].  offsets: experts + 1 ascending
- * values (device, as ft_expert_sort leaves them); values beyond rows count as rows, descending ones as empty groups.  Row r of C is of row
+ * values (device, as ft_expert_sort leaves them); values below 0 count as 0, values beyond rows as rows.  Where they are not ascending, no row is written that lies outside of
+ * 0 .. rows or in no offsets[e] .. offsets[e + 1] (one that ends before it begins holds none); what the others hold is unspecified.  Row r of C is of row
  * a_row[r] of A (device, e.g. row_token of ft_expert_sort: no gathered copy of A is needed), or of row r where a_row is NULL; A and
  * scale_a have a_rows rows, and a row outside of them counts as zeros.  Rows of C before offsets[0] and from offsets[experts] on are left as they were.
  * a_rows * lda < 2^31 and rows < 2^31, else FT_ERR_UNSUPPORTED.  rows = 0 launches nothing. */
