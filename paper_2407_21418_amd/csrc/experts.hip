@@ -364,9 +364,6 @@ template <int DT> MoveShape move_shape(const MoveArgs &a) {
     return s;
 }
 enum { MOVE_GATHER, MOVE_COMBINE, MOVE_GRAD };
-// Rows beyond what the last-level cache holds (256 MB) are streamed: 8192 tokens x 8 of 4096 bf16, all moves of a training step 640 us kept, 566
-// streamed; 1234 x 6 of 1001 fp16 the rows stay for the next call: combine 7.0 us kept, 8.4 streamed.
-constexpr uint64_t kStreamBytes = 256ull << 20;
 template <int DT, bool STREAM> ft_status move_launch(int what, MoveArgs a, hipStream_t stream) {
     const MoveShape s = move_shape<DT>(a);
     const uint32_t per = 256u / s.lanes, most = launch_rows(per, 256u);
@@ -389,7 +386,7 @@ template <int DT, bool STREAM> ft_status move_launch(int what, MoveArgs a, hipSt
     }
 }
 template <int DT> ft_status move_launch(int what, const MoveArgs &a, hipStream_t stream) {
-    return (uint64_t)a.entries * a.cols * RowType<DT>::BYTES > kStreamBytes ? move_launch<DT, true>(what, a, stream) : move_launch<DT, false>(what, a, stream);
+    return move_streams(a, RowType<DT>::BYTES) ? move_launch<DT, true>(what, a, stream) : move_launch<DT, false>(what, a, stream);
 }
 ft_status move(int what, const ft_expert_desc *desc, const MoveArgs &a, void *stream) {
     const ft_status st = op_stream_check(stream);

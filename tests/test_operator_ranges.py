@@ -1,5 +1,5 @@
 """Where matmuls in 8-bit integers and moves of tokens reach, by the rules of their launches compiled for the CPU (g++): copies that begin inside their rows,
-launches that HIP takes."""
+launches that HIP takes, forms that large calls take."""
 import ctypes as C
 import os
 import shutil
@@ -16,6 +16,11 @@ extern "C" int kernel(unsigned m, unsigned n, unsigned k, int gated, int experts
     ftk::I8Args a{};
     a.m = m; a.n = n; a.k = k; a.gated = gated; a.experts = experts; a.cus = 256;
     return (int)ftk::i8_choose(a, experts > 0);
+}
+extern "C" int streamed(unsigned entries, unsigned cols, unsigned bytes) {
+    ftk::MoveArgs a{};
+    a.entries = entries; a.cols = cols;
+    return ftk::move_streams(a, bytes);
 }
 extern "C" unsigned most_rows(unsigned per, unsigned threads) { return ftk::launch_rows(per, threads); }
 // the first turn whose scalar offset is at or beyond the reduce axis' end, or that reads other tiles than all of them once; -1: none
@@ -96,3 +101,23 @@ def test_rows_by_expert_lie_within_2_gb(lda, a_rows, fits):
     with pytest.raises(ft.FtError) as e:
         call()
     assert e.value.status == ft.FT_ERR_UNSUPPORTED
+
+
+# tokens, top_k, experts, columns, bytes of a value: moves that are streamed
+STREAMED = [(17000, 8, 16, 1001, 2), (8500, 8, 16, 1001, 4), (4100, 8, 60, 4097, 2), (2450000, 8, 5, 7, 2), (4200000, 32, 3, 1, 4), (33000, 2, 128, 2048, 2)]
+
+
+def test_large_moves_are_streamed(rules):
+    for tokens, top_k, _, cols, size in STREAMED:
+        assert rules.streamed(tokens * top_k, cols, size), (tokens, cols)
+    assert not rules.streamed(1 << 18, 512, 2) and rules.streamed((1 << 18) + 1, 512, 2)
+
+
+# m, n, k, gates, experts: blocks of 64 x 64 whose results are 4 MB and more (in rows of whole blocks of 64 bytes they go through the L2) in 16 bits
+LARGE_RESULTS = [(33001, 64, 3574, False, 0), (66001, 32, 2100, False, 0), (66001, 64, 2100, True, 0), (33001, 64, 3574, False, 5), (66001, 64, 2100, True, 5), (66001, 32, 2100, False, 40)]
+
+
+def test_blocks_of_64_with_large_results(rules):
+    for m, n, k, gates, experts in LARGE_RESULTS:
+        assert rules.kernel(m, n, k, int(gates), experts) == 1, (m, n, k, gates, experts)
+        assert 2 * m * (n // 2 if gates else n) >= 4 << 20
