@@ -394,50 +394,58 @@ def ft_launch_timed(p: Plan, A, B, Cs, stream: int, iters: int, graph: bool = Fa
     return ms.value
 
 
+def _number(n, what, bits=32):
+    """n, if it is one that the library's type holds (ctypes drops the bits that a type lacks: 2^32 rows would be none)."""
+    if isinstance(n, int) and not 0 <= n < 1 << bits:
+        raise FtError(FT_ERR_INVALID_ARG if n < 0 else FT_ERR_UNSUPPORTED, what)
+    return n
+
+
 def ft_i8_quantize(desc: ft_quant_desc, rows: int, X: int, Q: int, scale: int, stream: int = 0):
     """Rows of values at X as 8-bit integers at Q with one fp32 scale each.  All addresses here and below: device
     addresses (0 / None for none); stream: hipStream_t value."""
-    _check(lib().ft_i8_quantize(C.byref(desc), rows, X, Q, scale, stream), "ft_i8_quantize")
+    _check(lib().ft_i8_quantize(C.byref(desc), _number(rows, "ft_i8_quantize"), X, Q, scale, stream), "ft_i8_quantize")
 
 
 def ft_i8_matmul(desc: ft_i8_desc, m: int, A: int, scale_a: int, B: int, scale_b: int, bias: int, Cptr: int, stream: int = 0):
     """C[i, j] = scale_a[i] * scale_b[j] * sum_k A[i, k] B[j, k] (+ bias[j]) of 8-bit integers; B is stored [n][k]."""
-    _check(lib().ft_i8_matmul(C.byref(desc), m, A, scale_a, B, scale_b, bias or None, Cptr, stream), "ft_i8_matmul")
+    _check(lib().ft_i8_matmul(C.byref(desc), _number(m, "ft_i8_matmul"), A, scale_a, B, scale_b, bias or None, Cptr, stream), "ft_i8_matmul")
 
 
 def ft_i8_matmul_experts(desc: ft_i8_desc, rows: int, offsets: int, A: int, scale_a: int, a_row: int, a_rows: int, B: int, scale_b: int, bias: int,
                          Cptr: int, stream: int = 0):
     """The same where rows offsets[e] .. offsets[e + 1] of C belong to weight e; row r is of row a_row[r] of A (a_row 0: of row r)."""
-    _check(lib().ft_i8_matmul_experts(C.byref(desc), rows, offsets, A, scale_a, a_row or None, a_rows, B, scale_b, bias or None, Cptr, stream),
+    _check(lib().ft_i8_matmul_experts(C.byref(desc), _number(rows, "ft_i8_matmul_experts"), offsets, A, scale_a, a_row or None, _number(a_rows, "ft_i8_matmul_experts"), B, scale_b, bias or None, Cptr, stream),
            "ft_i8_matmul_experts")
 
 
 def ft_expert_workspace(desc: ft_expert_desc, tokens: int) -> int:
     """Bytes of workspace of ft_expert_sort."""
     n = u64()
-    _check(lib().ft_expert_workspace(C.byref(desc), tokens, C.byref(n)), "ft_expert_workspace")
+    _check(lib().ft_expert_workspace(C.byref(desc), _number(tokens, "ft_expert_workspace"), C.byref(n)), "ft_expert_workspace")
     return n.value
 
 
 def ft_expert_sort(desc: ft_expert_desc, tokens: int, expert_of: int, offsets: int, row_token: int, row_of: int, workspace: int, workspace_bytes: int,
                    stream: int = 0):
     """Rows of the entries sorted by expert: where each expert's begin, the token of each row, the row of each entry."""
-    _check(lib().ft_expert_sort(C.byref(desc), tokens, expert_of, offsets, row_token, row_of, workspace or None, workspace_bytes, stream), "ft_expert_sort")
+    _check(lib().ft_expert_sort(C.byref(desc), _number(tokens, "ft_expert_sort"), expert_of, offsets, row_token, row_of, workspace or None,
+                                _number(workspace_bytes, "ft_expert_sort", 64), stream), "ft_expert_sort")
 
 
 def ft_expert_gather(desc: ft_expert_desc, tokens: int, X: int, row_of: int, Y: int, stream: int = 0):
     """Y[row_of[t, j]] = X[t]."""
-    _check(lib().ft_expert_gather(C.byref(desc), tokens, X, row_of, Y, stream), "ft_expert_gather")
+    _check(lib().ft_expert_gather(C.byref(desc), _number(tokens, "ft_expert_gather"), X, row_of, Y, stream), "ft_expert_gather")
 
 
 def ft_expert_combine(desc: ft_expert_desc, tokens: int, Y: int, row_of: int, weights: int, Out: int, stream: int = 0):
     """Out[t] = sum_j weights[t, j] * Y[row_of[t, j]] (weights 0: ones)."""
-    _check(lib().ft_expert_combine(C.byref(desc), tokens, Y, row_of, weights or None, Out, stream), "ft_expert_combine")
+    _check(lib().ft_expert_combine(C.byref(desc), _number(tokens, "ft_expert_combine"), Y, row_of, weights or None, Out, stream), "ft_expert_combine")
 
 
 def ft_expert_combine_grad(desc: ft_expert_desc, tokens: int, dOut: int, Y: int, row_of: int, weights: int, dY: int, dweights: int, stream: int = 0):
     """Gradients of ft_expert_combine by Y and by the weights (dweights 0: not wanted, Y is not read then)."""
-    _check(lib().ft_expert_combine_grad(C.byref(desc), tokens, dOut, Y or None, row_of, weights or None, dY, dweights or None, stream), "ft_expert_combine_grad")
+    _check(lib().ft_expert_combine_grad(C.byref(desc), _number(tokens, "ft_expert_combine_grad"), dOut, Y or None, row_of, weights or None, dY, dweights or None, stream), "ft_expert_combine_grad")
 
 
 # A serving loop makes these for every Matmul or layer: the native ones read the usual arguments themselves and hand every other call to

@@ -33,6 +33,13 @@ bool address(PyObject *o, void **out) {
     *out = reinterpret_cast<void *>(static_cast<uintptr_t>(PyLong_AsUnsignedLongLongMask(o)));
     return true;
 }
+// a number of at most `bits` bits; ctypes would drop the others of a larger or negative one, and its functions are called for those
+bool number(PyObject *o, int bits, uint64_t *out) {
+    if (!PyLong_CheckExact(o)) return false;
+    *out = PyLong_AsUnsignedLongLong(o);
+    if (*out == ~0ull && PyErr_Occurred()) { PyErr_Clear(); return false; }
+    return bits == 64 || *out >> bits == 0;
+}
 bool pointer_of(PyObject *handle, void **out) {
     PyObject *p = PyObject_GetAttr(handle, s_ptr);
     if (!p) { PyErr_Clear(); return false; }                          // (the ctypes function raises it again)
@@ -126,9 +133,10 @@ struct Operator {
     op_thunk call;
     Py_ssize_t args;                     // descriptor and stream among them
     uint32_t numbers;                    // bit i: argument i is a number, not an address
+    int wide = 0;                        // the number that has 64 bits, where one has
 };
 constexpr Operator kOperators[kOps] = {
-    {"ft_i8_quantize", quantize, 6, 1u << 1},  {"ft_i8_matmul", matmul, 9, 1u << 1},   {"ft_i8_matmul_experts", matmul_experts, 12, 1u << 1 | 1u << 6}, {"ft_expert_sort", sort, 9, 1u << 1 | 1u << 7},
+    {"ft_i8_quantize", quantize, 6, 1u << 1},  {"ft_i8_matmul", matmul, 9, 1u << 1},   {"ft_i8_matmul_experts", matmul_experts, 12, 1u << 1 | 1u << 6}, {"ft_expert_sort", sort, 9, 1u << 1 | 1u << 7, 7},
     {"ft_expert_gather", gather, 6, 1u << 1},  {"ft_expert_combine", combine, 7, 1u << 1}, {"ft_expert_combine_grad", combine_grad, 9, 1u << 1}};
 void *g_op[kOps];
 PyObject *g_op_desc[kOps], *g_op_slow[kOps];
@@ -138,8 +146,12 @@ template <int I> PyObject *op(PyObject *, PyObject *const *a, Py_ssize_t n, PyOb
     uint64_t v[kOpArgs] = {};
     bool plain = g_op[I] && !kw && (n == o.args || n == o.args - 1) && (PyObject *)Py_TYPE(a[0]) == g_op_desc[I];
     for (Py_ssize_t i = 1; plain && i < n; ++i) {
+        if (o.numbers >> i & 1u) {
+            plain = number(a[i], i == o.wide ? 64 : 32, &v[i - 1]);
+            continue;
+        }
         void *p = nullptr;
-        plain = address(a[i], &p) && !(a[i] == Py_None && (o.numbers >> i & 1u));
+        plain = address(a[i], &p);
         v[i - 1] = reinterpret_cast<uintptr_t>(p);
     }
     if (!plain) return PyObject_Vectorcall(g_op_slow[I], a, n, kw);
