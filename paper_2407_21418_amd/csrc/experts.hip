@@ -5,12 +5,13 @@
 // of a workgroup has counts of its own for its stretch of the entries, and their prefix sums give each wave the row
 // where its next entry of an expert goes.  No atomic decides an order.
 //
-// Bound by latency: 8192 x 8 entries 4.7 and 7.1 us (counts, places), up to 16384 entries one launch, whose blocks count all of them:
-// 4 x 2 3.2 us, 1234 x 6 5.9.
+// Bound by latency: 8192 x 8 entries 9.9 us in a graph (counts and places 4.7 and 7.1 each by itself), up to 16384 entries one launch, whose blocks count all
+// of them: 4 x 2 3.3 us, 1234 x 6 5.9.
 //
 // The moves are bound by memory: a workgroup's threads hold a token's row in pieces of 16 bytes and read or write it once
 // for all of its entries; rows of entries are read or written once.  8192 x 8 of 4096 bf16: gather 119 us (5.1 TB/s), combine 110 (5.5), the
-// gradients 226 (5.1), where a copy reaches 4.8; 64 x 4 of 2048 2.7, 2.9 and 5.3 us, of which 2.1 are any launch's and its first read's.
+// gradients 226 (5.1), where a copy reaches 4.8; 64 x 4 of 2048 2.6, 2.9 and 5.3 us, of which 2.1 are any launch's and its first read's.  (The same
+// launch again and again in a graph; in a pass of several, whose rows another kernel has just left, small ones take up to a microsecond more.)
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

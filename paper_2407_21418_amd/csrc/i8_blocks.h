@@ -15,8 +15,9 @@ struct I8KindInfo {
     // few its tiles are; the second is what they share: the caches' bandwidth and the power.
     float once, round, round_k, tile, tile_k;
 };
-// Least squares over 348 shapes, m 8 .. 32768, n 768 .. 11008, k 64 .. 4096, all kinds measured at each (bf16 results, an idle device): the times
-// are met to 5 .. 13 % (root of the mean square), and the kind with the least is within 0.3 % of the fastest on average, 10 % at most.
+// Least squares over 348 shapes, m 8 .. 32768, n 768 .. 11008, k 64 .. 4096, all kinds measured at each (bf16 results, rows on whole blocks, an idle device): the times
+// are met to 5 .. 13 % (root of the mean square), and at those shapes the kind with the least is within 0.3 % of the fastest on average, 10 % at most.  Gates, a bias, fp32
+// results and longer reduce axes go by the same numbers, and results whose rows begin anywhere too, which cost a third more (403 x 1003 x 1001: 7.4 us for 5.7).
 constexpr I8KindInfo kI8Kinds[I8_KINDS] = {
     {16, 16, 1, 2.60f, 0.11f, 0.101f, 0.13f, 0.000f},
     {64, 64, 1, 2.92f, 1.22f, 0.141f, 0.57f, 0.053f},

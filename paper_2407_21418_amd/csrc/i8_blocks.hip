@@ -5,10 +5,10 @@
 // through its MFMAs, copies straight into LDS spread between them.  Both operands lie with k contiguous, so both are read with
 // ds_read_b128; chunks of 16 bytes are swizzled by their row.
 //
-// What bounds them: the largest blocks the matrix cores and the power they draw (8192 x 8192 x 8192 fp32 398 us, 2.76 POP/s, 8192 x 11008 x 4096
-// bf16 290 .. 330 by the clock; of 352k cycles of MFMAs for each SIMD the launch takes 620k: 5.4 rounds of blocks are 6, then what lies
+// What bounds them: the largest blocks the matrix cores and the power they draw (8192 x 8192 x 8192 fp32 398 .. 404 us, 2.76 POP/s, 8192 x 11008 x 4096
+// bf16 290 .. 337 by the clock; of 352k cycles of MFMAs for each SIMD the launch takes 620k: 5.4 rounds of blocks are 6, then what lies
 // between two blocks).  That is, of a 256 x 256 block's 56k cycles at K = 2048 with gates, 33k of MFMAs in 39k of products, 10k of scaling and
-// exponentials, 5k to the next tile's place and 2 .. 4k of its first copies (65536 x 2816 x 2048 gated 325 us, 38 of them for results).
+// exponentials, 5k to the next tile's place and 2 .. 4k of its first copies (65536 x 2816 x 2048 gated 322 us, 38 of them for results).
 // Smaller blocks are for fewer tiles than the device has places: 64 x 128 hides a latency behind two workgroups of a CU, 64 x 64 takes the reduce
 // axis in two groups of waves (256 x 768 x 768 4.9 us, 2.9 of them launch, first copies and results).
 #include <hip/hip_runtime.h>

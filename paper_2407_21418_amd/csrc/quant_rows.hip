@@ -1,8 +1,9 @@
 // Rows of values as 8-bit integers with one scale each, where asked after silu(gate) * up.
 //
 // Bound by memory: a row is read once, stays in its threads' registers while its largest magnitude is found, and
-// leaves as integers.  Rows of more than 32768 columns are read a second time.  65536 x 1408 fp32 82 us (5.6 TB/s), 8192 x 4096 bf16 20.8 (4.9),
-// 2048 x 2 x 11008 bf16 gated 24 (4.7), where a copy reaches 4.8; one row of 4096 2.8 us, most of which is any launch's.
+// leaves as integers.  Rows of more than 32768 columns are read a second time.  From memory 65536 x 1408 fp32 take 82 us (5.6 TB/s; 75 behind the
+// product that leaves a part of them in the last-level cache), 8192 x 4096 bf16 20.7 (4.9), 2048 x 2 x 11008 bf16 gated 24.6 (4.6), the same in
+// fp32 42.0 (4.8), 65536 x 2 x 1408 fp32 gated 154 (5.4), where a copy reaches 4.8; one row of 4096 2.8 us, most of which is any launch's.
 //
 // scale = amax / 127 and q = 127 f / amax to nearest even.  For 16-bit f this is exact without a division for each value: with 127 / amax
 // as the sum of two fp32, t = f * hi + f * lo is the quotient rounded once, 2^-24 of itself.  127 f / amax lies exactly in the middle
@@ -173,7 +174,7 @@ namespace {
 template <int DT, bool GATED> ft_status launch(QuantArgs a, hipStream_t s) {
     // Pieces of a thread: one where a few rows leave the device idle (16 x 4096 bf16 3.0 us, with two 3.25; from 1024 rows on alike), four where
     // more in flight is what wide rows lack (8192 x 4096 bf16 20.8 us, with two 22.1; 8192 x 11008 48.9 and 50.9), else two (65536 x 1408 fp32
-    // 81.0 us, with four 83.2; 2048 x 2 x 11008 gated 24.0 and 25.8; 8192 x 2048 bf16 12.7 and 13.6).
+    // 81.0 us, with four 83.2; 2048 x 2 x 11008 gated 24.0 and 25.8; 8192 x 2048 bf16 12.7 and 13.6; each pair on one card in turn).
     const uint32_t pieces = (a.cols + 7u) / 8u;
     const uint32_t hold = a.rows <= 256u ? 1u : !GATED && DT != ROW_F32 && a.cols >= 4096u ? 4u : 2u;
     uint32_t threads = ((pieces + hold - 1u) / hold + 63u) / 64u * 64u;
