@@ -6,9 +6,10 @@
 
 namespace ftk {
 
-// A kernel runs where its stream belongs: a stream of another device than the current one is refused.
+// A kernel runs where its stream belongs: a stream of another device than the current one is refused.  The default streams, by any of their handles, are the
+// current device's, and the latter two are no objects that could be asked.
 inline ft_status op_stream_check(void *stream) {
-    if (!stream) return FT_OK;
+    if (!stream || stream == static_cast<void *>(hipStreamLegacy) || stream == static_cast<void *>(hipStreamPerThread)) return FT_OK;
     int dev = -1;
     hipDevice_t of = -1;
     hipError_t e = hipGetDevice(&dev);
